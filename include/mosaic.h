@@ -29,6 +29,10 @@
  *    its infinity.
  *  - A cache holds num_seqs sequences x num_kv_heads kv heads.  Query head h
  *    of a sequence reads kv head h / group_size (GQA).
+ *  - Beside the paper's path: the rows that go into any of these caches
+ *    (mosaic_qk_norm_rope) and a cache of 8-bit codes with a scale for each
+ *    block of tokens and head (mosaic_quant_*), whose lengths live on the
+ *    device, so that captured calls follow them.
  */
 #ifndef MOSAIC_H
 #define MOSAIC_H
@@ -434,6 +438,112 @@ mosaic_status mosaic_dense_decode_attention(const void *q, const void *k, const 
                                             int32_t head_dim, int32_t dtype, int64_t seq_stride,
                                             int32_t max_ctx, const int32_t *ctx_lens, float sm_scale,
                                             void *ws, size_t ws_bytes, void *stream);
+
+/* Queries and keys of a model's projections, ready for a cache: each head's
+ * row x of 128 channels is normalised (with weights w: x / sqrt(mean(x^2) +
+ * eps) * w) and rotated to its token's position, in one pass; values can be
+ * laid out beside the keys.  The rotation turns pair i < rot_dim / 2 of
+ * channels by position * inv_freq[i]: channels (i, i + rot_dim / 2), or
+ * (2 i, 2 i + 1) when interleaved; channels from rot_dim on keep their place.
+ * Arithmetic is fp32 (the angle's turns fp64), rounded once to the dtype.
+ *   q, k, v      : rows in and out with element strides {sequence, token,
+ *                  head} (the 128 channels of a row are contiguous), e.g.
+ *                  views of one fused projection in, [num_seqs][kv_heads]
+ *                  [num_tokens][128] out.  v may be NULL; its rows are copied.
+ *                  An output may be its own input (same pointer and strides);
+ *                  otherwise nothing may overlap.  Pointers are 16-byte
+ *                  aligned, strides multiples of 8.
+ *   q_weight, k_weight : [128] of the dtype, 16-byte aligned; both NULL: no
+ *                  norm, rotation alone
+ *   positions    : int32 (pos_bytes 4) or int64 (8) at sequence * pos_strides
+ *                  [0] + token * pos_strides[1] elements (0: shared); exact
+ *                  up to 2^53
+ *   inv_freq     : fp32 [rot_dim / 2]; rot_dim is a multiple of 16 up to 128
+ * Strides are host arrays.  num_seqs or num_tokens 0: OK, nothing enqueued.
+ * Errors: INVALID (NULL, shape, alignment, strides), UNSUPPORTED (head_dim
+ * != 128, rot_dim, more than 2^31 - 1 tokens). */
+typedef struct {
+    const void *in;
+    void *out;
+    int64_t in_strides[3], out_strides[3];
+} mosaic_rows;
+mosaic_status mosaic_qk_norm_rope(const mosaic_rows *q, const mosaic_rows *k, const mosaic_rows *v, int32_t num_seqs,
+                                  int32_t num_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                                  const void *q_weight, const void *k_weight, float eps, const void *positions,
+                                  int32_t pos_bytes, const int64_t *pos_strides_host, const float *inv_freq,
+                                  int32_t rot_dim, int32_t interleaved, void *stream);
+
+/* A KV cache in 8 bits with one scale for each block of block_len tokens of a
+ * (sequence, kv head), K and V apart.  For a block x of tokens x 128 channels:
+ * a = max(max |x|, 2^-100), scale = a / Q, code = nearest(x * (Q / a)), ties to
+ * even, with Q = 448 (OCP FP8 E4M3) or 127 (8-bit integers); quotients and
+ * product are fp32.  A block is encoded once, when its last token arrives;
+ * until then its tokens are kept in 16 bits (the tail), so a cache's contents
+ * depend on its tokens and not on the calls that brought them.  A block also
+ * has bounds of its keys: per channel ceil of the largest and floor of the
+ * smallest k * (127 / a), 8-bit integers, and their unit a / 127.
+ *
+ * The caller owns every array; all are contiguous.  S = num_seqs, H =
+ * num_kv_heads, N = max_blocks, B = block_len (32 or 64); room is N B tokens a
+ * sequence.  lens must start at zero; setting a sequence's entries to zero (or
+ * all of them) empties it.  What lies behind a sequence's last block or token
+ * is never read and left as it was.  K and V must be finite; a value that is
+ * not spoils its own (sequence, kv head) only. */
+typedef enum { MOSAIC_E4M3 = 0, MOSAIC_INT8 = 1 } mosaic_code_format;
+typedef struct {
+    int32_t num_seqs, num_kv_heads, group_size, head_dim;  /* head_dim 128, group_size 1..8 */
+    int32_t dtype;                     /* mosaic_dtype of tokens, tails and queries */
+    int32_t format;                    /* mosaic_code_format */
+    int32_t block_len, max_blocks;
+    void *k;                           /* codes [S][H][N][B][128], 16-byte aligned */
+    void *v;                           /* codes [S][H][N][128][B] (by channel), 16-byte aligned */
+    float *k_scale, *v_scale, *bound_scale;  /* [S][H][N] */
+    int8_t *bounds;                    /* [S][H][N][2][128]: upper, lower; 16-byte aligned */
+    void *k_tail;                      /* [S][H][B][128] of the dtype, 16-byte aligned */
+    void *v_tail;                      /* [S][H][128][B] of the dtype, 16-byte aligned */
+    int32_t *lens;                     /* [S][H] tokens held (a sequence's entries are equal) */
+    int32_t *refused;                  /* [S] appends that a sequence had no room for */
+} mosaic_quant_cache;
+
+/* Appends tokens to every sequence: new_lens[s] of them (DEVICE int32 [S],
+ * values outside 0..max_new count as the nearest), or max_new each with NULL.
+ *   k, v : rows of 128 at sequence * strides[0] + kv head * strides[1] + token *
+ *          strides[2] elements (host arrays, multiples of 8), 16-byte aligned;
+ *          rows from new_lens[s] on are not read
+ * The lengths are known on the device only: a sequence that has no room for all
+ * of its new tokens takes none of them, and its entry of `refused` counts up.
+ * Errors: INVALID, UNSUPPORTED (head_dim, block_len), CAPACITY (max_new exceeds
+ * a sequence's room with new_lens NULL). */
+mosaic_status mosaic_quant_append(const mosaic_quant_cache *cache, const void *k, const void *v,
+                                  const int64_t *k_strides_host, const int64_t *v_strides_host, const int32_t *new_lens,
+                                  int32_t max_new, void *stream);
+
+/* Workspace of the two attentions below (depends on the cache's shape only).
+ * Calls that overlap on one workspace race; separate streams need their own. */
+mosaic_status mosaic_quant_workspace_bytes(const mosaic_quant_cache *cache, size_t *bytes);
+
+/* Decode attention over every token of the cache (dequantised codes, and the
+ * tail), one query token a sequence.
+ *   q   : [S][H * group_size][128] (cache dtype), 16-byte aligned
+ *   out : [S][H * group_size][128] fp32
+ *   ws  : at least mosaic_quant_workspace_bytes bytes, 256-byte aligned
+ * A sequence without tokens gets zeros. */
+mosaic_status mosaic_quant_decode_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,
+                                            void *ws, size_t ws_bytes, void *stream);
+
+/* The same over a selection of the blocks, and the tail.  A pair of nb whole
+ * blocks takes n = min(nb, max(1, ceil(nb select_num / select_den))) of them, by
+ * (score descending, index ascending).  A block's score bounds the products of
+ * its keys with the query: for each head q8 = nearest(q * (127 / aq)), aq =
+ * max(max |q|, 2^-100); I = sum over channels of q8 * (upper bound where q8 > 0,
+ * else lower), a whole number; the largest over the group's heads of float(I) *
+ * (aq / 127), times the block's bound_scale, in fp32.
+ *   blocks : NULL, or int32 [S][H][N]: receives the blocks taken, ascending,
+ *            then -1
+ * Errors: INVALID (also select_num < 1 or select_den < select_num). */
+mosaic_status mosaic_quant_select_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,
+                                            int32_t select_num, int32_t select_den, int32_t *blocks, void *ws,
+                                            size_t ws_bytes, void *stream);
 
 /* Memory accounting of Sec. 6.3 (reads the device state: synchronizes the
  * given stream).  used_bytes counts packed tokens, block keys, descriptors

@@ -10,10 +10,10 @@ from __future__ import annotations
 import ctypes as C
 from dataclasses import dataclass
 
-from ._lib import (OP_APPEND, OP_COMPRESS, OP_DECODE, OP_WINDOW_ROTATIONS, MosaicError, MosaicLayout, MosaicParams, MosaicStats,
-                   MosaicWsLayout, check, load)
+from ._lib import (OP_APPEND, OP_COMPRESS, OP_DECODE, OP_WINDOW_ROTATIONS, MosaicError, MosaicLayout, MosaicParams,
+                   MosaicQuantCache, MosaicRows, MosaicStats, MosaicWsLayout, check, load)
 
-__all__ = ["Params", "MosaicCache", "dense_decode", "MosaicError", "load"]
+__all__ = ["Params", "MosaicCache", "QuantParams", "QuantCache", "dense_decode", "qk_norm_rope", "MosaicError", "load"]
 
 D = 128
 
@@ -378,3 +378,250 @@ def reorder_rotations(params: Params, k, v, ctx_lens, max_tokens: int, rot_k, ro
         check(lib.mosaic_reorder_rotations(C.byref(p), S, max_tokens, _ptr(k), _ptr(v), stride, lens, _ptr(rot_k),
                                            _ptr(rot_v), _ptr(ws), ws.numel(), _stream(k.device)))
     return rot_k, rot_v
+
+
+def _on(device):
+    """The device made current for the calls inside (nothing to do where it is already)."""
+    import contextlib
+
+    import torch
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _strides3(t):
+    return (C.c_int64 * 3)(*t.stride()[:3])
+
+
+def _rows(t, name, shape, dtype, device):
+    """t, checked: rows of 128 contiguous channels, 16-byte aligned, in any order."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}: the channels of a row must be contiguous")
+    return t
+
+
+def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, v=None,
+                 q_out=None, k_out=None, v_out=None):
+    """Norm of each query and key head (with weights) and rotation to the
+    tokens' positions, in one pass, laid out for the caches.
+
+    q [S][n][Hq][128], k and v [S][n][Hkv][128]: views of any strides with
+    contiguous channels (fp16 or bf16), e.g. of one fused projection;
+    positions [S][n] int32 or int64 (any strides); inv_freq fp32 [R / 2], R a
+    multiple of 16: pair i turns by positions * inv_freq[i], pairs being
+    channels (i, i + R / 2) or, interleaved, (2 i, 2 i + 1).  q_weight and
+    k_weight [128] or neither.  Returns q_out [S][n][Hq][128], k_out
+    [S][Hkv][n][128] and with v also v_out [S][Hkv][n][128] (v's rows as they
+    are): new tensors, or the given ones, which may be views of any strides.
+    An output may be its own input's memory, row for row; otherwise nothing may
+    overlap."""
+    import torch
+    if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k are tensors [S][n][heads][128]")
+    dev, dt = q.device, q.dtype
+    if dev.type != "cuda":
+        raise ValueError("q must be on a GPU")
+    if dt not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"q has dtype {dt}, expected float16 or bfloat16")
+    S, n, hq, _ = q.shape
+    hkv = k.shape[2]
+    _rows(q, "q", (S, n, hq, D), dt, dev)
+    _rows(k, "k", (S, n, hkv, D), dt, dev)
+    if q_out is None:
+        q_out = torch.empty((S, n, hq, D), dtype=dt, device=dev)
+    else:
+        _rows(q_out, "q_out", (S, n, hq, D), dt, dev)
+    if k_out is None:
+        k_out = torch.empty((S, hkv, n, D), dtype=dt, device=dev)
+    else:
+        _rows(k_out, "k_out", (S, hkv, n, D), dt, dev)
+    if not isinstance(positions, torch.Tensor) or positions.dtype not in (torch.int32, torch.int64):
+        raise ValueError("positions must be an int32 or int64 tensor")
+    if positions.device != dev or tuple(positions.shape) != (S, n):
+        raise ValueError(f"positions: shape {tuple(positions.shape)} on {positions.device}, expected {(S, n)} on {dev}")
+    _check_tensor(inv_freq, "inv_freq", torch.float32, dev)
+    if inv_freq.dim() != 1:
+        raise ValueError("inv_freq must have one dimension")
+    if (q_weight is None) != (k_weight is None):
+        raise ValueError("give both weights or neither")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _check_tensor(w, name, dt, dev)
+            if tuple(w.shape) != (D,):
+                raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {(D,)}")
+
+    def rows(a, b, swap):
+        ao, bo = a.stride(), b.stride()
+        order = (bo[0], bo[2], bo[1]) if swap else bo[:3]
+        return MosaicRows(a.data_ptr(), b.data_ptr(), (C.c_int64 * 3)(*ao[:3]), (C.c_int64 * 3)(*order))
+    vr = None
+    if v is not None:
+        _rows(v, "v", (S, n, hkv, D), dt, dev)
+        if v_out is None:
+            v_out = torch.empty((S, hkv, n, D), dtype=dt, device=dev)
+        else:
+            _rows(v_out, "v_out", (S, hkv, n, D), dt, dev)
+        vr = C.byref(rows(v, v_out, True))
+    elif v_out is not None:
+        raise ValueError("v_out without v")
+    if S and n:
+        with _on(dev):
+            check(load().mosaic_qk_norm_rope(C.byref(rows(q, q_out, False)), C.byref(rows(k, k_out, True)), vr, S, n, hq, hkv, D,
+                                             1 if dt == torch.bfloat16 else 0, _ptr(q_weight), _ptr(k_weight), float(eps),
+                                             _ptr(positions), positions.element_size(), (C.c_int64 * 2)(*positions.stride()),
+                                             _ptr(inv_freq), 2 * inv_freq.numel(), int(interleaved), _stream(dev)))
+    return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+
+@dataclass
+class QuantParams:
+    """Shape of an 8-bit cache: codes ("e4m3" or "int8") with one scale for each
+    block of `block` (32 or 64) tokens and kv head."""
+    num_kv_heads: int = 8
+    group_size: int = 4
+    dtype: str = "fp16"
+    format: str = "e4m3"
+    block: int = 32
+
+
+class QuantCache:
+    """One layer's KV cache in 8 bits for `num_seqs` sequences of up to
+    max_tokens tokens (rounded up to whole blocks).
+
+    The cache is its tensors (attributes; S sequences, H kv heads, N blocks of B
+    tokens): codes k [S][H][N][B][128] and v [S][H][N][128][B], k_scale, v_scale
+    and bound_scale [S][H][N], bounds [S][H][N][2][128], the 16-bit tokens of
+    the unfinished blocks k_tail [S][H][B][128] and v_tail [S][H][128][B], and
+    lens [S][H].  tensors: a dict of these to use in place of new ones (all, or
+    some).  Lengths live on the device: nothing here synchronizes, and captured
+    calls follow them.  Calls on one cache must be ordered (one stream, or
+    events); they share its workspace."""
+
+    TENSORS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens")
+
+    def __init__(self, params: QuantParams, num_seqs: int, max_tokens: int, device="cuda", tensors=None):
+        import torch
+        self.lib = load()
+        self.params, self.num_seqs = params, num_seqs
+        if params.dtype not in ("fp16", "bf16"):
+            raise ValueError(f"dtype {params.dtype!r}: fp16 or bf16")
+        if params.format not in ("e4m3", "int8"):
+            raise ValueError(f"format {params.format!r}: e4m3 or int8")
+        if params.block not in (32, 64):
+            raise ValueError(f"block {params.block}: 32 or 64")
+        if num_seqs < 1 or max_tokens < 1:
+            raise ValueError(f"num_seqs {num_seqs}, max_tokens {max_tokens}")
+        given = dict(tensors or {})
+        if set(given) - set(self.TENSORS):
+            raise ValueError(f"unknown tensors {sorted(set(given) - set(self.TENSORS))}")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            at = next((t.device for t in given.values() if isinstance(t, torch.Tensor) and t.device.type == "cuda"), None)
+            self.device = at or torch.device("cuda", torch.cuda.current_device())
+        self.elem = torch.bfloat16 if params.dtype == "bf16" else torch.float16
+        S, H, B, N = num_seqs, params.num_kv_heads, params.block, -(-max_tokens // params.block)
+        self.max_tokens = N * B
+        code = torch.int8 if params.format == "int8" else torch.float8_e4m3fn
+        shapes = dict(k=((N, B, D), code), v=((N, D, B), code), k_scale=((N,), torch.float32), v_scale=((N,), torch.float32),
+                      bound_scale=((N,), torch.float32), bounds=((N, 2, D), torch.int8), k_tail=((B, D), self.elem),
+                      v_tail=((D, B), self.elem), lens=((), torch.int32))
+        self._c = MosaicQuantCache(S, H, params.group_size, D, 1 if params.dtype == "bf16" else 0, 1 if params.format == "int8" else 0,
+                                   B, N)
+        n = C.c_size_t()
+        check(self.lib.mosaic_quant_workspace_bytes(C.byref(self._c), C.byref(n)))
+        for name, (tail, dtype) in shapes.items():
+            t = given.get(name)
+            if t is None:
+                make = torch.zeros if name == "lens" else torch.empty
+                t = make((S, H) + tail, dtype=dtype, device=self.device)
+            _check_tensor(t, name, dtype, self.device)
+            if tuple(t.shape) != (S, H) + tail:
+                raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(S, H) + tail}")
+            setattr(self, name, t)
+            setattr(self._c, name, t.data_ptr())
+        #: appends that each sequence had no room for (it took none of their tokens)
+        self.refused = torch.zeros(S, dtype=torch.int32, device=self.device)
+        self._c.refused = self.refused.data_ptr()
+        self.workspace = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self._cp = C.byref(self._c)
+
+    def tensors(self) -> dict:
+        return {n: getattr(self, n) for n in self.TENSORS}
+
+    def reset(self, seqs=None):
+        """Empties the cache, or the sequences of an index tensor or list."""
+        import torch
+        if seqs is None:
+            self.lens.zero_()
+        else:
+            self.lens[torch.as_tensor(seqs, dtype=torch.long, device=self.device)] = 0
+
+    def append(self, k, v, new_lens=None):
+        """k, v: [S][H][n][128] or [S][H][128] (one token), any strides with
+        contiguous channels; new_lens: int32 [S] on the GPU, how many of its n
+        tokens each sequence takes (None: all)."""
+        import torch
+        S, H = self.num_seqs, self.params.num_kv_heads
+        if isinstance(k, torch.Tensor) and isinstance(v, torch.Tensor) and k.dim() == 3 and v.dim() == 3:
+            k, v = k.unsqueeze(2), v.unsqueeze(2)
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be a tensor [S][H][n][128]")
+        shape = (S, H, k.shape[2], D)
+        _rows(k, "k", shape, self.elem, self.device)
+        _rows(v, "v", shape, self.elem, self.device)
+        if new_lens is not None:
+            _check_tensor(new_lens, "new_lens", torch.int32, self.device)
+            if tuple(new_lens.shape) != (S,):
+                raise ValueError(f"new_lens has shape {tuple(new_lens.shape)}, expected {(S,)}")
+        if shape[2] == 0:
+            return
+        with _on(self.device):
+            check(self.lib.mosaic_quant_append(self._cp, _ptr(k), _ptr(v), _strides3(k), _strides3(v), _ptr(new_lens), shape[2],
+                                               _stream(self.device)))
+        self._keep = (k, v, new_lens)  # alive until the enqueued work completes
+
+    def _query(self, q, out):
+        import torch
+        shape = (self.num_seqs, self.params.num_kv_heads * self.params.group_size, D)
+        _check_tensor(q, "q", self.elem, self.device)
+        if tuple(q.shape) != shape:
+            raise ValueError(f"q shape {tuple(q.shape)} != {shape}")
+        if out is None:
+            return torch.empty(shape, dtype=torch.float32, device=self.device)
+        _check_tensor(out, "out", torch.float32, self.device)
+        if tuple(out.shape) != shape:
+            raise ValueError(f"out shape {tuple(out.shape)} != {shape}")
+        return out
+
+    def decode(self, q, sm_scale: float, out=None):
+        """Attention over every token: q [S][H * G][128] -> fp32 [S][H * G][128]."""
+        out = self._query(q, out)
+        with _on(self.device):
+            check(self.lib.mosaic_quant_decode_attention(self._cp, _ptr(q), _ptr(out), float(sm_scale), _ptr(self.workspace),
+                                                         self.workspace.numel(), _stream(self.device)))
+        return out
+
+    def decode_selected(self, q, sm_scale: float, select=(1, 10), out=None, blocks=None):
+        """Attention over the share select = (num, den) of each (sequence, kv
+        head)'s whole blocks whose key bounds promise the largest logits, and
+        its unfinished block.  blocks: int32 [S][H][N], receives the blocks
+        taken, ascending, then -1."""
+        import torch
+        out = self._query(q, out)
+        if blocks is not None:
+            _check_tensor(blocks, "blocks", torch.int32, self.device)
+            if blocks.shape != self.k_scale.shape:
+                raise ValueError(f"blocks shape {tuple(blocks.shape)} != {tuple(self.k_scale.shape)}")
+        with _on(self.device):
+            check(self.lib.mosaic_quant_select_attention(self._cp, _ptr(q), _ptr(out), float(sm_scale), int(select[0]), int(select[1]),
+                                                         _ptr(blocks), _ptr(self.workspace), self.workspace.numel(),
+                                                         _stream(self.device)))
+        return out

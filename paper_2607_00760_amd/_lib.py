@@ -19,7 +19,8 @@ EXPORTED = [
     "mosaic_set_timing", "mosaic_decode_timing", "mosaic_rotation_workspace_bytes", "mosaic_compute_rotations",
     "mosaic_reorder_workspace_bytes", "mosaic_reorder_rotations", "mosaic_decode_attention_noalloc",
     "mosaic_window_poll", "mosaic_window_close", "mosaic_cache_create_ragged", "mosaic_cache_pair_regions",
-    "mosaic_window_rotations",
+    "mosaic_window_rotations", "mosaic_qk_norm_rope", "mosaic_quant_append", "mosaic_quant_workspace_bytes",
+    "mosaic_quant_decode_attention", "mosaic_quant_select_attention",
 ]
 
 
@@ -51,6 +52,16 @@ class MosaicWsLayout(C.Structure):
         "selinfo_stride", "wres_off", "wres_stride", "total")] + [
         ("max_blocks", C.c_int32), ("max_splits", C.c_int32), ("gp", C.c_int32), ("reserved", C.c_int32),
         ("tkx_off", C.c_uint64), ("tkx_stride", C.c_uint64)]
+
+
+class MosaicRows(C.Structure):
+    _fields_ = [("inp", C.c_void_p), ("out", C.c_void_p), ("in_strides", C.c_int64 * 3), ("out_strides", C.c_int64 * 3)]
+
+
+class MosaicQuantCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("num_seqs", "num_kv_heads", "group_size", "head_dim", "dtype", "format", "block_len",
+                                         "max_blocks")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens", "refused")]
 
 
 class MosaicStats(C.Structure):
@@ -116,8 +127,19 @@ def bind_signatures(L: C.CDLL) -> C.CDLL:
     L.mosaic_seq_tokens.restype = C.c_int32
     L.mosaic_last_error.argtypes = []
     L.mosaic_last_error.restype = C.c_char_p
+    if hasattr(L, "mosaic_quant_append"):                   # (a library of the cache's host layer alone has the rest)
+        qc, st3 = C.POINTER(MosaicQuantCache), C.POINTER(C.c_int64)
+        rows = C.POINTER(MosaicRows)
+        L.mosaic_qk_norm_rope.argtypes = [rows, rows, rows] + [C.c_int32] * 6 + [vp, vp, C.c_float, vp, C.c_int32, st3, vp, C.c_int32,
+                                                                               C.c_int32, vp]
+        L.mosaic_quant_append.argtypes = [qc, vp, vp, st3, st3, vp, C.c_int32, vp]
+        L.mosaic_quant_workspace_bytes.argtypes = [qc, C.POINTER(sz)]
+        L.mosaic_quant_decode_attention.argtypes = [qc, vp, vp, C.c_float, vp, sz, vp]
+        L.mosaic_quant_select_attention.argtypes = [qc, vp, vp, C.c_float, C.c_int32, C.c_int32, vp, vp, sz, vp]
     for n in EXPORTED:
-        f = getattr(L, n)
+        f = getattr(L, n, None)
+        if f is None:
+            continue
         if f.restype is C.c_int:   # default restype -> mosaic_status
             f.restype = C.c_int32
     return L

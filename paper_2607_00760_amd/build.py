@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmosaic.so")
 ARCH = os.environ.get("MOSAIC_OFFLOAD_ARCH", "gfx950")
 SOURCES = ["api.hip", "attn_bf16_g4.hip", "attn_bf16_g8.hip", "attn_fp16_g4.hip", "attn_fp16_g8.hip", "compress.hip",
-           "decode.hip", "dense.hip", "encode.hip", "rotation.hip", "score.hip"]
+           "decode.hip", "dense.hip", "encode.hip", "norm_rope.hip", "quant_api.hip", "quant_append.hip", "quant_attn_e4m3.hip",
+           "quant_attn_int8.hip", "quant_select.hip", "rotation.hip", "score.hip"]
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -45,6 +45,8 @@ int ilog2(int v) { int l = 0; while ((1 << l) < v) ++l; return l; }
 
 }  // namespace
 
+void mosaic::set_last_error(const char *message) { g_err = message; }
+
 struct mosaic_cache {
     mosaic_params P;
     int num_seqs, max_tokens, rotated, npairs, GP, nw, max_desc, max_blocks, max_sel, max_splits;

@@ -241,6 +241,9 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// the message of mosaic_last_error on this thread (api.hip)
+void set_last_error(const char *message);
+
 // ---------------------------------------------------------------- launchers
 // (implemented in the .hip files; all return hipError_t of the launch)
 hipError_t launch_ctx_copy(int32_t *dst_dev, const int32_t *src_host, int n, hipStream_t s);
@@ -286,6 +289,19 @@ hipError_t launch_attn_fp16_g8(const Geom &g, const WsGeom &w, float scale, cons
 hipError_t launch_dense(const uint16_t *q, const uint16_t *k, const uint16_t *v, float *out, int nseq,
                         int hkv, int G, int dtype, int64_t seq_stride, int max_ctx, const int32_t *ctx,
                         float scale, float *part, hipStream_t s);
+
+// queries, keys and (v set) values of `seqs` sequences of n tokens
+struct NormRope {
+    struct Part { const uint16_t *in; uint16_t *out; int64_t in_seq, in_tok, in_head, out_seq, out_tok, out_head; };
+    Part q, k, vp;
+    const uint16_t *qw, *kw;              // weights, or null: no norm
+    const float *inv_freq;                // [half]
+    const void *pos;
+    int64_t pos_seq, pos_tok;
+    int seqs, n, hq, hkv, half, pos64, v;
+    float eps;
+};
+hipError_t launch_norm_rope(const NormRope &a, int dtype, int interleaved, hipStream_t s);
 
 size_t dense_part_bytes(int npairs, int G, int max_ctx);
 size_t rotation_ctx_bytes(int num_seqs);

@@ -1,0 +1,112 @@
+// quant.h -- shared by the kernels of the 8-bit KV cache (quant_append.hip,
+// quant_attn.hip, quant_select.hip) and by their entry points (quant_api.hip)
+// (not part of the C ABI).
+#pragma once
+#include "decode_common.h"
+
+namespace mosaic {
+
+constexpr float QLEAST = 7.888609052210118e-31f;          // 2^-100: magnitudes below count as this in a scale
+constexpr int QF_E4M3 = 0, QF_INT8 = 1;
+__host__ __device__ constexpr float q_top(int fmt) { return fmt == QF_INT8 ? 127.0f : 448.0f; }
+
+// The cache's tensors (mosaic_quant_cache), passed by value.
+struct QCache {
+    int S, H, G, N;                                        // sequences, kv heads, group, blocks of a pair at most
+    int cap;                                               // tokens of a sequence at most
+    uint8_t *k, *v;                                        // codes [S][H][N][B][D] and [S][H][N][D][B]
+    float *ks, *vs, *bs;                                   // scales of K, V and bounds [S][H][N]
+    int8_t *bounds;                                        // [S][H][N][2][D]: upper, lower
+    uint16_t *kt, *vt;                                     // unfinished block [S][H][B][D] and [S][H][D][B]
+    int32_t *lens;                                         // [S][H]: a pair's workgroups need no other pair's
+    int32_t *refused;                                      // [S]: appends that a sequence had no room for
+    // a pair's length; one that no append can have left reads as the nearest that can
+    __device__ __forceinline__ int len(long long p) const { return min(max(lens[p], 0), cap); }
+};
+
+struct QNew {                                              // tokens to append, strides in elements
+    const uint16_t *k, *v;
+    int64_t k_seq, k_head, k_tok, v_seq, v_head, v_tok;
+    const int32_t *counts;                                 // [S] on the device, or null: max_new each
+    int max_new;
+};
+
+// How a launch of about `slots` workgroups shares the units of all pairs: runs
+// of c units, c a multiple of cmin, that do not cross pairs.  The lengths are
+// read on the device, so a captured launch follows them; runs are equal
+// however ragged the batch, and there are at most slots + pairs of them.
+struct QPlan {
+    int s, h, i, ns;                                       // sequence, kv head, run of the pair, runs of the pair
+    int c, L, first;                                       // units of a run, the sequence's tokens, the pair's first run
+    bool live;
+};
+
+// units(L): units of a pair of L tokens; least: runs of a pair with tokens at
+// least.  w < 0: the pair `pair`'s plan (its run 0); else run w's.
+template <typename U>
+__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int least, U units, int w, int pair) {
+    const int lane = threadIdx.x & 63;
+    uint32_t total = 0;
+    for (int s0 = 0; s0 < q.S; s0 += 64) {
+        const int s = s0 + lane;
+        total += s < q.S ? (uint32_t)units(q.len((long long)s * q.H)) : 0u;
+    }
+    total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(total), 63) * (uint32_t)q.H;
+    const uint32_t c0 = (total + (uint32_t)slots - 1u) / (uint32_t)slots;
+    const int c = max(cmin, (int)((c0 + (uint32_t)cmin - 1u) / (uint32_t)cmin) * cmin);
+    QPlan p{};
+    p.c = c;
+    uint32_t base = 0;
+    const int want = pair / q.H;
+    for (int s0 = 0; s0 < q.S; s0 += 64) {
+        const int s = s0 + lane;
+        const int L = s < q.S ? q.len((long long)s * q.H) : 0;
+        const int ns = L > 0 ? max(least, (units(L) + c - 1) / c) : 0;
+        const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
+        uint64_t hit;
+        if (w >= 0) hit = __ballot(base + inc > (uint32_t)w);          // the first sequence whose runs end past w
+        else hit = __ballot(s == want);
+        if (hit) {
+            const int l = (int)__builtin_ctzll(hit);
+            p.s = s0 + l;
+            p.ns = __builtin_amdgcn_readlane(ns, l);
+            p.L = __builtin_amdgcn_readlane(L, l);
+            p.first = (int)(base + (uint32_t)__builtin_amdgcn_readlane((int)inc, l)) - p.ns * q.H;
+            if (w >= 0) {
+                const int r = w - p.first;
+                p.h = r / p.ns;
+                p.i = r - p.h * p.ns;
+            } else {
+                p.h = pair - p.s * q.H;
+            }
+            p.first += p.h * p.ns;
+            p.live = true;
+            return p;
+        }
+        base += (uint32_t)__builtin_amdgcn_readlane((int)inc, 63);
+    }
+    return p;
+}
+
+// blocks of a pair of L tokens that a selection takes
+__host__ __device__ __forceinline__ int q_want(int whole, int num, int den) {
+    const long long n = ((long long)whole * num + den - 1) / den;
+    return (int)(n < 1 ? (whole < 1 ? whole : 1) : (n > whole ? whole : n));
+}
+
+struct QSel {                                              // a selection, or list = null: every block
+    int num, den;
+    const int32_t *list;                                   // [pairs][N] ascending
+};
+
+// ---------------------------------------------------------------- launchers
+hipError_t launch_quant_append(const QCache &q, int fmt, int block, int dtype, const QNew &n, hipStream_t s);
+size_t quant_part_bytes(int pairs);                        // the attention's partials
+hipError_t launch_quant_attn_e4m3(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
+                                  float *part, float *out, hipStream_t s);
+hipError_t launch_quant_attn_int8(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
+                                  float *part, float *out, hipStream_t s);
+hipError_t launch_quant_select(const QCache &q, int block, int dtype, const uint16_t *query, int num, int den, float *scores,
+                               int32_t *list, hipStream_t s);
+
+}  // namespace mosaic

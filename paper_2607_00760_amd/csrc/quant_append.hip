@@ -1,0 +1,208 @@
+// quant_append.hip -- tokens into the 8-bit KV cache (mosaic_quant_append).
+//
+// A block of B tokens of one (sequence, kv head) gets one scale for its keys
+// and one for its values: a = max(max |x|, 2^-100), scale = a / Q, code =
+// nearest(x * (Q / a)).  It is encoded once, when its last token arrives, from
+// 16-bit tokens; until then its tokens wait in the tail, so the codes do not
+// depend on how many calls brought the tokens.  A block's key bounds (per
+// channel the largest and the smallest key, in units of a / 127, rounded
+// outwards) come from the same registers.
+//
+// One workgroup per (block that the call may complete, pair): half of it takes
+// the keys, half the values, a thread 4 tokens x 8 channels.  The values'
+// codes are stored by channel, 4 x 4 bytes turned in registers.  HBM is the
+// bound: 512 bytes of a token are read, 256 and the block's share are written.
+#include <type_traits>
+
+#include "quant.h"
+
+namespace mosaic {
+
+namespace {
+
+// bytes e of four words: the columns of a 4 x 4 byte matrix
+__device__ __forceinline__ void turn4(const uint32_t (&r)[4], uint32_t (&c)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+    const uint32_t d = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), e = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+    c[0] = __builtin_amdgcn_perm(d, a, 0x05040100u);
+    c[1] = __builtin_amdgcn_perm(d, a, 0x07060302u);
+    c[2] = __builtin_amdgcn_perm(e, b, 0x05040100u);
+    c[3] = __builtin_amdgcn_perm(e, b, 0x07060302u);
+}
+
+// codes of four values already in units of the scale, one byte each
+template <int FMT> __device__ __forceinline__ uint32_t codes4(const float (&y)[4]) {
+    if (FMT == QF_E4M3) {
+        float z[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = __builtin_amdgcn_fmed3f(y[i], -448.0f, 448.0f);
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], w, true);
+    }
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(y[i]), -127.0f, 127.0f) & 0xffu) << (8 * i);
+    return w;
+}
+
+// grid (blocks that the call may complete, pairs).  solo: the grid has one
+// block, so its workgroup is the only one that needs the length and writes it.
+template <int FMT, int B, int DT>
+__global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw, int solo) {
+    constexpr int HW = 4 * B / 64;                             // waves of a half
+    __shared__ float red[2 * HW];
+    __shared__ float bnd[HW][16][16];                          // [wave][8 upper, 8 lower of 8 channels][channel group]
+    const int p = blockIdx.y, j = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int s = p / q.H, h = p - s * q.H;
+    const int vals = tid >= 4 * B, t4 = (tid & (4 * B - 1)) >> 4, pc = tid & 15;
+    const int L = q.len(p);
+    int n = nw.counts ? nw.counts[s] : nw.max_new;
+    n = min(max(n, 0), nw.max_new);
+    if (n == 0) return;
+    if (n > q.cap - L) {               // no room: the sequence stays as it is
+        if (j == 0 && h == 0 && tid == 0) q.refused[s] += 1;
+        return;
+    }
+    const int f = L % B, first = L / B, done = (f + n) / B;
+    if (j > 0 && j >= done) return;
+    const uint16_t *src = vals ? nw.v + s * nw.v_seq + h * nw.v_head : nw.k + s * nw.k_seq + h * nw.k_head;
+    const int64_t tok = vals ? nw.v_tok : nw.k_tok;
+    uint16_t *kt = q.kt + (uint64_t)p * B * D, *vt = q.vt + (uint64_t)p * B * D;
+    if (j < done) {
+        uint4 x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int c = j * B + 4 * t4 + r;                  // token of the unfinished block and the new ones together
+            if (c >= f) x[r] = *(const uint4 *)(src + (int64_t)(c - f) * tok + 8 * pc);
+            else if (!vals) x[r] = *(const uint4 *)(kt + c * D + 8 * pc);
+            else {
+                uint16_t e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = vt[(8 * pc + i) * B + c];
+                __builtin_memcpy(&x[r], e, 16);
+            }
+        }
+        float y[4][8];
+        float a = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t w[4] = {x[r].x, x[r].y, x[r].z, x[r].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                y[r][i] = h2f((uint16_t)((i & 1) ? (w[i >> 1] >> 16) : w[i >> 1]), DT);
+                a = fmaxf(a, fabsf(y[r][i]));
+            }
+        }
+        a = wave_max(a);
+        if (lane == 0) red[wave] = a;
+        if (!vals) {                                           // the channels' largest and smallest keys of the wave
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float hi = fmaxf(fmaxf(y[0][i], y[1][i]), fmaxf(y[2][i], y[3][i]));
+                const float lo = fminf(fminf(y[0][i], y[1][i]), fminf(y[2][i], y[3][i]));
+                const float u = rows_all(hi, [](float m, float o) { return fmaxf(m, o); });
+                const float d = rows_all(lo, [](float m, float o) { return fminf(m, o); });
+                if (lane < 16) { bnd[wave][i][pc] = u; bnd[wave][8 + i][pc] = d; }
+            }
+        }
+        __syncthreads();
+        a = red[vals * HW];
+#pragma unroll
+        for (int w = 1; w < HW; ++w) a = fmaxf(a, red[vals * HW + w]);
+        a = fmaxf(a, QLEAST);
+        const float inv = q_top(FMT) / a;
+        const uint64_t blk = (uint64_t)p * q.N + first + j;
+        if (tid == 4 * B) q.vs[blk] = a / q_top(FMT);
+        if (tid == 0) { q.ks[blk] = a / q_top(FMT); q.bs[blk] = a / 127.0f; }
+        uint32_t c[4][2];                                      // [token][channels 0..3, 4..7]
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float z[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = y[r][4 * e + i] * inv;
+                c[r][e] = codes4<FMT>(z);
+            }
+        if (!vals) {
+            uint8_t *kp = q.k + blk * (B * D);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) *(uint2 *)(kp + (4 * t4 + r) * D + 8 * pc) = make_uint2(c[r][0], c[r][1]);
+            if (tid < D) {                                     // (a half has at least as many threads as channels)
+                const float unit = 127.0f / a;
+                float hi = bnd[0][tid & 7][tid >> 3], lo = bnd[0][8 + (tid & 7)][tid >> 3];
+#pragma unroll
+                for (int w = 1; w < HW; ++w) {
+                    hi = fmaxf(hi, bnd[w][tid & 7][tid >> 3]);
+                    lo = fminf(lo, bnd[w][8 + (tid & 7)][tid >> 3]);
+                }
+                int8_t *bp = q.bounds + blk * (2 * D);
+                bp[tid] = (int8_t)(int)__builtin_amdgcn_fmed3f(ceilf(hi * unit), -127.0f, 127.0f);
+                bp[D + tid] = (int8_t)(int)__builtin_amdgcn_fmed3f(floorf(lo * unit), -127.0f, 127.0f);
+            }
+        } else {
+            uint8_t *vp = q.v + blk * (B * D) + 4 * t4;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t r[4] = {c[0][e], c[1][e], c[2][e], c[3][e]};
+                uint32_t o[4];
+                turn4(r, o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *(uint32_t *)(vp + (8 * pc + 4 * e + i) * B) = o[i];
+            }
+        }
+    }
+    if (j > 0) return;
+    // the tokens that no block holds yet: from here on the tail's old rows have
+    // been read (the barrier above), or stay where they are
+    const int rest = f + n - done * B, t0 = done ? 0 : f;
+    for (int i = tid; i < (rest - t0) * 16; i += 8 * B) {
+        const int t = t0 + (i >> 4), g = i & 15;
+        const int64_t at = (int64_t)(done * B + t - f);
+        const uint4 kx = *(const uint4 *)(nw.k + s * nw.k_seq + h * nw.k_head + at * nw.k_tok + 8 * g);
+        const uint4 vx = *(const uint4 *)(nw.v + s * nw.v_seq + h * nw.v_head + at * nw.v_tok + 8 * g);
+        *(uint4 *)(kt + t * D + 8 * g) = kx;
+        const uint32_t w[4] = {vx.x, vx.y, vx.z, vx.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vt[(8 * g + e) * B + t] = (uint16_t)((e & 1) ? (w[e >> 1] >> 16) : w[e >> 1]);
+    }
+    if (solo) {
+        __syncthreads();                                       // every thread has read the length
+        if (tid == 0) q.lens[p] = L + n;
+    }
+}
+
+// the lengths after a call whose pairs had several workgroups
+__global__ void __launch_bounds__(256) k_quant_lens(QCache q, QNew nw) {
+    const int p = blockIdx.x * 256 + threadIdx.x;
+    if (p >= q.S * q.H) return;
+    const int L = q.len(p), n = min(max(nw.counts ? nw.counts[p / q.H] : nw.max_new, 0), nw.max_new);
+    if (n <= q.cap - L) q.lens[p] = L + n;
+}
+
+}  // namespace
+
+hipError_t launch_quant_append(const QCache &q, int fmt, int block, int dtype, const QNew &n, hipStream_t s) {
+    const int most = (block - 1 + n.max_new) / block, solo = most <= 1;
+    const int pairs = q.S * q.H;
+    const dim3 grid(most < 1 ? 1 : most, pairs);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(8 * block), 0, s, q, n, solo); };
+    auto by_type = [&](auto f, auto b) {
+        constexpr int F = decltype(f)::value, B = decltype(b)::value;
+        if (dtype) go(k_quant_append<F, B, 1>); else go(k_quant_append<F, B, 0>);
+    };
+    using std::integral_constant;
+    if (fmt == QF_INT8) {
+        if (block == 32) by_type(integral_constant<int, QF_INT8>{}, integral_constant<int, 32>{});
+        else by_type(integral_constant<int, QF_INT8>{}, integral_constant<int, 64>{});
+    } else {
+        if (block == 32) by_type(integral_constant<int, QF_E4M3>{}, integral_constant<int, 32>{});
+        else by_type(integral_constant<int, QF_E4M3>{}, integral_constant<int, 64>{});
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || solo) return e;
+    hipLaunchKernelGGL(k_quant_lens, dim3(ceil_div(pairs, 256)), dim3(256), 0, s, q, n);
+    return hipGetLastError();
+}
+
+}  // namespace mosaic

@@ -1,0 +1,343 @@
+// quant_attn.h -- attention over the 8-bit KV cache, every block or a
+// selection (mosaic_quant_decode_attention, mosaic_quant_select_attention);
+// one source per code format (quant_attn_*.hip).
+//
+// out = sum_t p_t v_t / sum_t p_t, p_t = exp(scale q.k_t - max), with k_t and
+// v_t their codes times their block's scale.  One pass with running maximum
+// and sum: a wave takes a block at a time, straight from memory into matrix
+// operands.  Both products are fp16: a code of either format is an fp16 value,
+// a query of 8 or 11 bits too (bf16 after a power of two per head), and the
+// weights take part as two fp16 parts, 22 bits, in rows 0..7 and 8..15 of the
+// left operand, which groups of up to 8 heads leave room for.  A block's value
+// scale goes into its weights, relative to the largest scale so far.
+//
+// The products' layouts ask for 8 tokens of one channel in a lane: values lie
+// by channel in the cache, and the rows of the first product are dealt so that
+// a lane's logits are consecutive tokens (token (B / 4) (row / 4) + 4 tile +
+// row % 4), so no value passes through LDS.
+//
+// HBM is the bound: 256 bytes of a token, with the next block's loads out
+// while one is worked on.
+#pragma once
+#include "quant.h"
+
+namespace mosaic {
+
+namespace {
+
+constexpr int QA_NWV = 4;                                  // waves of a workgroup
+constexpr int QA_RUNS = 1024;                              // runs of a launch, about
+constexpr int QA_HEADS = 8;
+constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: max, sum, accumulators
+
+// 8 codes as fp16
+template <int FMT> __device__ __forceinline__ dhf8 codes_f16(uint32_t a, uint32_t b) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 h2;
+    h2 o[4];
+    const uint32_t w[2] = {a, b};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (FMT == QF_E4M3) {
+            o[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, false);
+            o[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w[i], 1.0f, true);
+        } else {                                           // 1024 + (code + 128) has the code's bits, then - 1152
+            const uint32_t u = w[i] ^ 0x80808080u;
+            const h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+            o[2 * i] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
+            o[2 * i + 1] = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
+        }
+    }
+    dhf8 r;
+    __builtin_memcpy(&r, o, 16);
+    return r;
+}
+
+template <int FMT, int B> struct QStage {                  // a block in flight
+    uint4 k[B / 16][2];                                    // 16 channels of a token each
+    uint32_t v[8][B / 16];                                 // B / 4 tokens of a channel each
+    float ks, vs;
+};
+
+template <int FMT, int B, int DT, bool SEL>
+__global__ void __launch_bounds__(64 * QA_NWV) __attribute__((amdgpu_waves_per_eu(2)))
+k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, float *part) {
+    using DM = DMma<DT>;
+    constexpr int NT = B / 16, TPQ = B / 4;                // tiles of 16 tokens, tokens of a lane
+    constexpr float PS = 16384.0f;                         // small weights stay in fp16's normal range
+    __shared__ float mrg[QA_NWV][16][D + 2];
+    auto units = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
+    const QPlan pl = q_plan(q, QA_RUNS, QA_NWV, 1, units, blockIdx.x, 0);
+    if (!pl.live) return;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int p = pl.s * q.H + pl.h;
+    const int b0 = pl.i * pl.c, b1 = min(units(pl.L), b0 + pl.c), rest = pl.i == pl.ns - 1 ? pl.L % B : 0;
+    const int head = min(l16 & 7, q.G - 1);                // (columns past the group repeat its last head)
+    const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
+    // q operand: column l16 is head l16 % 8, inner index (j, half, q4, i) channel 64 j + 16 q4 + 8 half + i
+    dhf8 qb[4];
+    float zs;                                              // softmax scale in powers of two, and q's
+    {
+        float x[4][8], a = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint16_t w[8];
+            __builtin_memcpy(w, qp + 64 * (e >> 1) + 16 * q4 + 8 * (e & 1), 16);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { x[e][i] = h2f(w[i], DT); a = fmaxf(a, fabsf(x[e][i])); }
+        }
+        float down = 1.0f;
+        zs = scale * 1.44269504088896340736f;
+        if (DT) {                                          // largest magnitude in [1, 2), what falls below 2^-24 of it is lost
+            a = rows_all(a, [](float m, float o) { return fmaxf(m, o); });
+            const uint32_t e = min(max(__float_as_uint(a) >> 23, 1u), 253u);
+            down = __uint_as_float((254u - e) << 23);
+            zs *= __uint_as_float(e << 23);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) qb[e][i] = (_Float16)(x[e][i] * down);
+    }
+    float m_run = -INFINITY, l_run = 0.0f;                 // head l16 % 8; the sum over this lane's tokens only
+    float ref = 0.0f;                                      // a power of two above every value scale so far; the unit of acc
+    df4 acc[8];                                            // [channel tile][row 4 q4 + r]
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) acc[ct] = df4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto scale_acc = [&](const float (&f)[4]) {
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[ct][r] *= f[r];
+    };
+    // the softmax's step over logits z, to weights in units that make acc's
+    auto weigh = [&](float (&z)[NT][4], float vs) {
+        if (vs > ref) {
+            const float up = __uint_as_float((__float_as_uint(vs) & 0x7f800000u) + 0x00800000u), f = ref / up;
+            const float ff[4] = {f, f, f, f};
+            scale_acc(ff);
+            ref = up;
+        }
+        float cm = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) cm = fmaxf(cm, z[n][r]);
+        cm = rows_all(cm, [](float a, float b) { return fmaxf(a, b); });
+        const float mn = fmaxf(m_run, cm);
+        const float mb = mn == -INFINITY ? 0.0f : mn;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - mb);
+        float ls = 0.0f;
+        const float wf = ref > 0.0f ? vs * (PS / ref) : 0.0f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = __builtin_amdgcn_exp2f(z[n][r] - mb);
+                ls += e;
+                z[n][r] = e * wf;
+            }
+        l_run = fmaf(l_run, alpha, ls);
+        m_run = mn;
+        if (!__all(alpha == 1.0f)) {                       // some head's running maximum moved
+            float f[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {                  // alpha of head (4 q4 + r) % 8
+                const float a0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), r));
+                const float a1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), 4 + r));
+                f[r] = (q4 & 1) ? a1 : a0;
+            }
+            scale_acc(f);
+        }
+    };
+    const int32_t *list = SEL ? sel.list + (uint64_t)p * q.N : nullptr;
+    const uint64_t pb = (uint64_t)p * q.N;
+    auto load = [&](int t, QStage<FMT, B> &st) {
+        const uint64_t blk = pb + (uint32_t)(SEL ? list[t] : t);
+        const uint8_t *kp = q.k + blk * (B * D), *vp = q.v + blk * (B * D);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                st.k[n][j] = *(const uint4 *)(kp + (TPQ * (l16 >> 2) + 4 * n + (l16 & 3)) * D + 64 * j + 16 * q4);
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) __builtin_memcpy(st.v[ct], __builtin_assume_aligned(vp + (16 * ct + l16) * B + TPQ * q4, TPQ), TPQ);
+        st.ks = q.ks[blk];
+        st.vs = q.vs[blk];
+    };
+    auto consume = [&](const QStage<FMT, B> &st) {
+        float z[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            df4 a = df4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                a = DMma<0>::run(codes_f16<FMT>(st.k[n][j].x, st.k[n][j].y), qb[2 * j], a);
+                a = DMma<0>::run(codes_f16<FMT>(st.k[n][j].z, st.k[n][j].w), qb[2 * j + 1], a);
+            }
+            const float f = zs * st.ks;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[n][r] = a[r] * f;          // token TPQ q4 + 4 n + r, head l16 % 8
+        }
+        weigh(z, st.vs);
+#pragma unroll
+        for (int s = 0; s < B / 32; ++s) {
+            dhf8 pa;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = z[2 * s + (i >> 2)][i & 3];
+                const _Float16 hi = (_Float16)w;
+                pa[i] = l16 < 8 ? hi : (_Float16)(w - (float)hi);
+            }
+#pragma unroll
+            for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, codes_f16<FMT>(st.v[ct][2 * s], st.v[ct][2 * s + 1]), acc[ct]);
+        }
+    };
+    QStage<FMT, B> st0, st1;
+    int t = b0 + wave;
+    if (t < b1) load(t, st0);
+    while (t < b1) {                                       // (two steps a turn: no copies that would wait on the loads)
+        load(t + QA_NWV < b1 ? t + QA_NWV : t, st1);       // (the last step loads itself again)
+        __builtin_amdgcn_sched_barrier(0);
+        consume(st0);
+        t += QA_NWV;
+        if (t >= b1) break;
+        load(t + QA_NWV < b1 ? t + QA_NWV : t, st0);
+        __builtin_amdgcn_sched_barrier(0);
+        consume(st1);
+        t += QA_NWV;
+    }
+    if (rest && wave == ((b1 - b0) & (QA_NWV - 1))) {      // the unfinished block, in 16 bits
+        using M8 = typename DM::v8;
+        using E = typename DM::el;
+        const uint16_t *kp = q.kt + (uint64_t)p * B * D, *vp = q.vt + (uint64_t)p * B * D;
+        M8 qd[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) __builtin_memcpy(&qd[e], qp + 32 * e + 8 * q4, 16);
+        float z[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            df4 a = df4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                M8 x;
+                __builtin_memcpy(&x, kp + (TPQ * (l16 >> 2) + 4 * n + (l16 & 3)) * D + 32 * e + 8 * q4, 16);
+                a = DM::run(x, qd[e], a);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)                    // (rows behind the last token may hold anything)
+                z[n][r] = TPQ * q4 + 4 * n + r < rest ? a[r] * (scale * 1.44269504088896340736f) : -INFINITY;
+        }
+        weigh(z, 1.0f);
+#pragma unroll
+        for (int s = 0; s < B / 32; ++s) {
+            M8 pa, pl2{};                                  // bf16: a third part, its rows the first eight
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = z[2 * s + (i >> 2)][i & 3];
+                const E hi = (E)w;
+                const float r1 = w - (float)hi;
+                const E mid = (E)r1;
+                pa[i] = l16 < 8 ? hi : mid;
+                if (DT) pl2[i] = l16 < 8 ? (E)(r1 - (float)mid) : (E)0.0f;
+            }
+            const int keep = rest - (TPQ * q4 + 8 * s);    // tokens of the lane's eight
+#pragma unroll
+            for (int ct = 0; ct < 8; ++ct) {
+                uint4 x = *(const uint4 *)(vp + (16 * ct + l16) * B + TPQ * q4 + 8 * s);
+                x.x = keep >= 2 ? x.x : (keep == 1 ? x.x & 0xffffu : 0u);
+                x.y = keep >= 4 ? x.y : (keep == 3 ? x.y & 0xffffu : 0u);
+                x.z = keep >= 6 ? x.z : (keep == 5 ? x.z & 0xffffu : 0u);
+                x.w = keep >= 8 ? x.w : (keep == 7 ? x.w & 0xffffu : 0u);
+                const M8 vb = __builtin_bit_cast(M8, x);
+                acc[ct] = DM::run(pa, vb, acc[ct]);
+                if (DT) acc[ct] = DM::run(pl2, vb, acc[ct]);
+            }
+        }
+    }
+    // join the waves
+    l_run = rows_all(l_run, [](float a, float b) { return a + b; });
+    const float back = ref * (1.0f / PS);
+    if (lane < 16) { mrg[wave][l16][0] = m_run; mrg[wave][l16][1] = l_run; }
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mrg[wave][4 * q4 + r][2 + 16 * ct + l16] = acc[ct][r] * back;
+    __syncthreads();
+    float *out = part + (uint64_t)blockIdx.x * QA_PART;
+    for (int i = tid; i < q.G * D; i += 64 * QA_NWV) {
+        const int h = i / D, c = i % D;
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < QA_NWV; ++w) M = fmaxf(M, mrg[w][h][0]);
+        float A = 0.0f, S = 0.0f;
+#pragma unroll
+        for (int w = 0; w < QA_NWV; ++w) {
+            const float f = mrg[w][h][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mrg[w][h][0] - M);
+            A += (mrg[w][h][2 + c] + mrg[w][h + 8][2 + c]) * f;
+            S += mrg[w][h][1] * f;
+        }
+        out[2 * QA_HEADS + i] = A;
+        if (c == 0) { out[h] = M; out[QA_HEADS + h] = S; }
+    }
+}
+
+// grid (pairs, columns of a pair's outputs / 256): the runs of a pair joined in order
+template <bool SEL>
+__global__ void __launch_bounds__(256) k_quant_combine(QCache q, QSel sel, int block, const float *part, float *out) {
+    constexpr int CB = 16;
+    const int p = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x, h = i / D;
+    const QPlan pl = q_plan(q, QA_RUNS, QA_NWV, 1, [&](int L) { return SEL ? q_want(L / block, sel.num, sel.den) : L / block; }, -1, p);
+    if (i >= q.G * D) return;
+    float M = -INFINITY, S = 0.0f, A = 0.0f;
+    for (int s0 = 0; s0 < pl.ns; s0 += CB) {
+        float m[CB], l[CB], a[CB];
+#pragma unroll
+        for (int e = 0; e < CB; ++e) {
+            if (s0 + e < pl.ns) {
+                const float *ps = part + (uint64_t)(pl.first + s0 + e) * QA_PART;
+                m[e] = ps[h];
+                l[e] = ps[QA_HEADS + h];
+                a[e] = ps[2 * QA_HEADS + i];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < CB; ++e) {
+            if (s0 + e < pl.ns && m[e] != -INFINITY) {
+                const float mn = fmaxf(M, m[e]);
+                const float x = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(m[e] - mn);
+                A = A * x + a[e] * y;
+                S = S * x + l[e] * y;
+                M = mn;
+            }
+        }
+    }
+    out[(uint64_t)p * q.G * D + i] = S > 0.0f ? A / S : (S != S ? S : 0.0f);
+}
+
+}  // namespace
+
+template <int FMT>
+hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
+                               float *part, float *out, hipStream_t s) {
+    const int pairs = q.S * q.H;
+    const int blocks = sel.list ? q_want(q.N, sel.num, sel.den) : q.N;
+    const long long most = (long long)pairs * ceil_div(blocks, QA_NWV);
+    const dim3 grid((uint32_t)(most < QA_RUNS + pairs ? most : QA_RUNS + pairs));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * QA_NWV), 0, s, q, sel, query, scale, part); };
+    if (sel.list) {
+        if (block == 32) { if (dtype) go(k_quant_attn<FMT, 32, 1, true>); else go(k_quant_attn<FMT, 32, 0, true>); }
+        else { if (dtype) go(k_quant_attn<FMT, 64, 1, true>); else go(k_quant_attn<FMT, 64, 0, true>); }
+    } else {
+        if (block == 32) { if (dtype) go(k_quant_attn<FMT, 32, 1, false>); else go(k_quant_attn<FMT, 32, 0, false>); }
+        else { if (dtype) go(k_quant_attn<FMT, 64, 1, false>); else go(k_quant_attn<FMT, 64, 0, false>); }
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 cgrid(pairs, ceil_div(q.G * D, 256));
+    if (sel.list) hipLaunchKernelGGL(k_quant_combine<true>, cgrid, dim3(256), 0, s, q, sel, block, part, out);
+    else hipLaunchKernelGGL(k_quant_combine<false>, cgrid, dim3(256), 0, s, q, sel, block, part, out);
+    return hipGetLastError();
+}
+
+}  // namespace mosaic
