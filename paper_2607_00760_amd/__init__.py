@@ -550,7 +550,7 @@ class QuantCache:
         #: appends that each sequence had no room for (it took none of their tokens)
         self.refused = torch.zeros(S, dtype=torch.int32, device=self.device)
         self._c.refused = self.refused.data_ptr()
-        self.workspace = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=self.device)
         self._cp = C.byref(self._c)
 
     def tensors(self) -> dict:

@@ -37,14 +37,13 @@ struct QNew {                                              // tokens to append, 
 // however ragged the batch, and there are at most slots + pairs of them.
 struct QPlan {
     int s, h, i, ns;                                       // sequence, kv head, run of the pair, runs of the pair
-    int c, L, first;                                       // units of a run, the sequence's tokens, the pair's first run
+    int c, L;                                              // units of a run, the sequence's tokens
     bool live;
 };
 
-// units(L): units of a pair of L tokens; least: runs of a pair with tokens at
-// least.  w < 0: the pair `pair`'s plan (its run 0); else run w's.
+// units(L): units of a pair of L tokens; least: runs of a pair at least.
 template <typename U>
-__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int least, U units, int w, int pair) {
+__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int least, U units, int w) {
     const int lane = threadIdx.x & 63;
     uint32_t total = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
@@ -57,29 +56,20 @@ __device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, in
     QPlan p{};
     p.c = c;
     uint32_t base = 0;
-    const int want = pair / q.H;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
         const int s = s0 + lane;
         const int L = s < q.S ? q.len((long long)s * q.H) : 0;
-        const int ns = L > 0 ? max(least, (units(L) + c - 1) / c) : 0;
+        const int ns = s < q.S ? max(least, (units(L) + c - 1) / c) : 0;
         const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
-        uint64_t hit;
-        if (w >= 0) hit = __ballot(base + inc > (uint32_t)w);          // the first sequence whose runs end past w
-        else hit = __ballot(s == want);
+        const uint64_t hit = __ballot(base + inc > (uint32_t)w);       // the first sequence whose runs end past w
         if (hit) {
             const int l = (int)__builtin_ctzll(hit);
             p.s = s0 + l;
             p.ns = __builtin_amdgcn_readlane(ns, l);
             p.L = __builtin_amdgcn_readlane(L, l);
-            p.first = (int)(base + (uint32_t)__builtin_amdgcn_readlane((int)inc, l)) - p.ns * q.H;
-            if (w >= 0) {
-                const int r = w - p.first;
-                p.h = r / p.ns;
-                p.i = r - p.h * p.ns;
-            } else {
-                p.h = pair - p.s * q.H;
-            }
-            p.first += p.h * p.ns;
+            const int r = w - ((int)(base + (uint32_t)__builtin_amdgcn_readlane((int)inc, l)) - p.ns * q.H);
+            p.h = r / p.ns;
+            p.i = r - p.h * p.ns;
             p.live = true;
             return p;
         }
@@ -101,11 +91,15 @@ struct QSel {                                              // a selection, or li
 
 // ---------------------------------------------------------------- launchers
 hipError_t launch_quant_append(const QCache &q, int fmt, int block, int dtype, const QNew &n, hipStream_t s);
-size_t quant_part_bytes(int pairs);                        // the attention's partials
+constexpr int Q_PAIRS = 65535;                             // pairs at most
+// the attention's workspace: arrivals [Q_PAIRS + 1] (zero between calls), then partials
+size_t quant_attn_ws_bytes(int pairs);
 hipError_t launch_quant_attn_e4m3(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
-                                  float *part, float *out, hipStream_t s);
+                                  void *ws, float *out, hipStream_t s);
 hipError_t launch_quant_attn_int8(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
-                                  float *part, float *out, hipStream_t s);
+                                  void *ws, float *out, hipStream_t s);
+// scores: [pairs][q_score_stride(N)]
+__host__ __device__ __forceinline__ int q_score_stride(int n) { return (n + 3) & ~3; }
 hipError_t launch_quant_select(const QCache &q, int block, int dtype, const uint16_t *query, int num, int den, float *scores,
                                int32_t *list, hipStream_t s);
 

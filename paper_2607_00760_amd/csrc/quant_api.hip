@@ -40,7 +40,7 @@ mosaic_status quant_shape(const mosaic_quant_cache *c) {
         return fail(MOSAIC_ERR_INVALID, "num_seqs %d, num_kv_heads %d, group_size %d, max_blocks %d", c->num_seqs, c->num_kv_heads,
                     c->group_size, c->max_blocks);
     const long long pairs = (long long)c->num_seqs * c->num_kv_heads;
-    if (pairs > 65535) return fail(MOSAIC_ERR_UNSUPPORTED, "%lld (sequence, kv head) pairs: at most 65535", pairs);
+    if (pairs > Q_PAIRS) return fail(MOSAIC_ERR_UNSUPPORTED, "%lld (sequence, kv head) pairs: at most %d", pairs, Q_PAIRS);
     if ((long long)c->max_blocks * c->block_len > 0x3fffffff || pairs * c->max_blocks > 0x3fffffff)
         return fail(MOSAIC_ERR_UNSUPPORTED, "%d blocks of %d tokens for %lld pairs", c->max_blocks, c->block_len, pairs);
     return MOSAIC_OK;
@@ -61,13 +61,13 @@ mosaic_status quant_arrays(const mosaic_quant_cache *c, QCache &q) {
     return MOSAIC_OK;
 }
 
-struct QuantWs { uint64_t scores, list, total; };          // partials first
+struct QuantWs { uint64_t scores, list, total; };          // the attention's part first
 QuantWs quant_ws(const mosaic_quant_cache *c) {
-    const uint64_t pairs = (uint64_t)c->num_seqs * c->num_kv_heads, n = pairs * c->max_blocks * 4;
+    const uint64_t pairs = (uint64_t)c->num_seqs * c->num_kv_heads;
     QuantWs w;
-    w.scores = align256(quant_part_bytes((int)pairs));
-    w.list = w.scores + align256(n);
-    w.total = w.list + align256(n);
+    w.scores = align256(quant_attn_ws_bytes((int)pairs));
+    w.list = w.scores + align256(pairs * q_score_stride(c->max_blocks) * 4);
+    w.total = w.list + align256(pairs * c->max_blocks * 4);
     return w;
 }
 
@@ -85,7 +85,7 @@ mosaic_status attend_args(const mosaic_quant_cache *c, const void *q, const floa
 hipError_t attend(const mosaic_quant_cache *c, const QCache &qc, const void *q, float *out, float scale, const QSel &sel, void *ws,
                   void *stream) {
     const auto f = c->format == MOSAIC_INT8 ? launch_quant_attn_int8 : launch_quant_attn_e4m3;
-    return f(qc, c->block_len, c->dtype, (const uint16_t *)q, scale, sel, (float *)ws, out, (hipStream_t)stream);
+    return f(qc, c->block_len, c->dtype, (const uint16_t *)q, scale, sel, ws, out, (hipStream_t)stream);
 }
 
 bool bad_strides(const int64_t *s) { return (s[0] | s[1] | s[2]) % 8 != 0; }

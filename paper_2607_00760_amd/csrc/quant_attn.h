@@ -26,7 +26,9 @@ namespace mosaic {
 namespace {
 
 constexpr int QA_NWV = 4;                                  // waves of a workgroup
-constexpr int QA_RUNS = 1024;                              // runs of a launch, about
+// Runs of a launch: with up to 256 pairs they and the pairs' rounding fill the
+// 512 workgroups that the chip holds once; more pairs take several rounds anyway.
+__host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256 ? 512 - pairs : 1024; }
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: max, sum, accumulators
 
@@ -58,15 +60,73 @@ template <int FMT, int B> struct QStage {                  // a block in flight
     float ks, vs;
 };
 
+__device__ __forceinline__ float joined(float a, float s) { return s > 0.0f ? a / s : (s != s ? s : 0.0f); }
+
+// partials, past the XCD's L2
+__device__ __forceinline__ void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float2 get2(const float *p) {
+    return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// The partials of ns runs to a pair's outputs: a thread takes four columns of
+// every np-th run, np = 256 / (32 G) shares, joined in LDS.  The loads of 8
+// runs are out together.
+__device__ __forceinline__ void join_runs(const float *part, int ns, int G, float *lds, float *out) {
+    constexpr int CB = 8;
+    const int tid = threadIdx.x, cols = 32 * G, np = 64 * QA_NWV / cols;
+    const int share = tid / cols, col = tid - share * cols, h = col >> 5;
+    float M = -INFINITY, S = 0.0f;
+    float4 A = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](float m, float l, float4 a) {
+        if (m == -INFINITY) return;
+        const float mn = fmaxf(M, m);
+        const float x = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(m - mn);
+        A = make_float4(A.x * x + a.x * y, A.y * x + a.y * y, A.z * x + a.z * y, A.w * x + a.w * y);
+        S = S * x + l * y;
+        M = mn;
+    };
+    if (share < np)
+        for (int r0 = share; r0 < ns; r0 += CB * np) {
+            float m[CB], l[CB];
+            float4 a[CB];
+#pragma unroll
+            for (int e = 0; e < CB; ++e) {
+                const float *ps = part + (uint64_t)min(r0 + e * np, ns - 1) * QA_PART;
+                m[e] = get(ps + h);
+                l[e] = get(ps + QA_HEADS + h);
+                const float2 lo = get2(ps + 2 * QA_HEADS + 4 * col), hi = get2(ps + 2 * QA_HEADS + 4 * col + 2);
+                a[e] = make_float4(lo.x, lo.y, hi.x, hi.y);
+            }
+#pragma unroll
+            for (int e = 0; e < CB; ++e)
+                if (r0 + e * np < ns) add(m[e], l[e], a[e]);
+        }
+    float *x = lds + 8 * tid;
+    if (share > 0 && share < np) {
+        *(float4 *)x = A;
+        x[4] = M;
+        x[5] = S;
+    }
+    __syncthreads();
+    if (share > 0) return;
+    for (int e = 1; e < np; ++e) {
+        const float *y = lds + 8 * (tid + e * cols);
+        add(y[4], y[5], *(const float4 *)y);
+    }
+    *(float4 *)(out + 4 * col) = make_float4(joined(A.x, S), joined(A.y, S), joined(A.z, S), joined(A.w, S));
+}
+
 template <int FMT, int B, int DT, bool SEL>
 __global__ void __launch_bounds__(64 * QA_NWV) __attribute__((amdgpu_waves_per_eu(2)))
-k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, float *part) {
+k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *arrivals, float *part, float *outp) {
     using DM = DMma<DT>;
     constexpr int NT = B / 16, TPQ = B / 4;                // tiles of 16 tokens, tokens of a lane
     constexpr float PS = 16384.0f;                         // small weights stay in fp16's normal range
-    __shared__ float mrg[QA_NWV][16][D + 2];
+    __shared__ __align__(16) float mrg[QA_NWV][16][D + 2];
+    __shared__ int last;
     auto units = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
-    const QPlan pl = q_plan(q, QA_RUNS, QA_NWV, 1, units, blockIdx.x, 0);
+    const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_NWV, 1, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -264,7 +324,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, float *part
 #pragma unroll
         for (int r = 0; r < 4; ++r) mrg[wave][4 * q4 + r][2 + 16 * ct + l16] = acc[ct][r] * back;
     __syncthreads();
-    float *out = part + (uint64_t)blockIdx.x * QA_PART;
+    float *out = outp + (uint64_t)p * q.G * D;
+    // partials of a pair's runs are consecutive: run 0's is this workgroup's less pl.i
+    float *mine = part + (uint64_t)blockIdx.x * QA_PART;
     for (int i = tid; i < q.G * D; i += 64 * QA_NWV) {
         const int h = i / D, c = i % D;
         float M = -INFINITY;
@@ -277,54 +339,42 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, float *part
             A += (mrg[w][h][2 + c] + mrg[w][h + 8][2 + c]) * f;
             S += mrg[w][h][1] * f;
         }
-        out[2 * QA_HEADS + i] = A;
-        if (c == 0) { out[h] = M; out[QA_HEADS + h] = S; }
-    }
-}
-
-// grid (pairs, columns of a pair's outputs / 256): the runs of a pair joined in order
-template <bool SEL>
-__global__ void __launch_bounds__(256) k_quant_combine(QCache q, QSel sel, int block, const float *part, float *out) {
-    constexpr int CB = 16;
-    const int p = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x, h = i / D;
-    const QPlan pl = q_plan(q, QA_RUNS, QA_NWV, 1, [&](int L) { return SEL ? q_want(L / block, sel.num, sel.den) : L / block; }, -1, p);
-    if (i >= q.G * D) return;
-    float M = -INFINITY, S = 0.0f, A = 0.0f;
-    for (int s0 = 0; s0 < pl.ns; s0 += CB) {
-        float m[CB], l[CB], a[CB];
-#pragma unroll
-        for (int e = 0; e < CB; ++e) {
-            if (s0 + e < pl.ns) {
-                const float *ps = part + (uint64_t)(pl.first + s0 + e) * QA_PART;
-                m[e] = ps[h];
-                l[e] = ps[QA_HEADS + h];
-                a[e] = ps[2 * QA_HEADS + i];
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < CB; ++e) {
-            if (s0 + e < pl.ns && m[e] != -INFINITY) {
-                const float mn = fmaxf(M, m[e]);
-                const float x = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(m[e] - mn);
-                A = A * x + a[e] * y;
-                S = S * x + l[e] * y;
-                M = mn;
-            }
+        if (pl.ns == 1) {
+            out[i] = joined(A, S);
+        } else {
+            put(mine + 2 * QA_HEADS + i, A);
+            if (c == 0) { put(mine + h, M); put(mine + QA_HEADS + h, S); }
         }
     }
-    out[(uint64_t)p * q.G * D + i] = S > 0.0f ? A / S : (S != S ? S : 0.0f);
+    if (pl.ns == 1) return;
+    // The pair's last workgroup joins its runs, in their order whichever it is.
+    // Partials are written and read past the XCD's L2 (agent scope): once a
+    // wave's stores are acknowledged every XCD reads them.  (A release fence in
+    // their place writes back the whole L2, 6 us a launch and more.)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+        const bool l = __hip_atomic_fetch_add(&arrivals[p], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pl.ns - 1u;
+        if (l) __hip_atomic_store(&arrivals[p], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = l;
+    }
+    __syncthreads();
+    if (!last) return;
+    join_runs(part + (uint64_t)(blockIdx.x - pl.i) * QA_PART, pl.ns, q.G, &mrg[0][0][0], out);
 }
 
 }  // namespace
 
 template <int FMT>
 hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
-                               float *part, float *out, hipStream_t s) {
-    const int pairs = q.S * q.H;
+                               void *ws, float *out, hipStream_t s) {
+    const int pairs = q.S * q.H, runs = qa_runs(pairs) + pairs;
+    uint32_t *arrivals = (uint32_t *)ws;
+    float *part = (float *)(arrivals + Q_PAIRS + 1);
     const int blocks = sel.list ? q_want(q.N, sel.num, sel.den) : q.N;
     const long long most = (long long)pairs * ceil_div(blocks, QA_NWV);
-    const dim3 grid((uint32_t)(most < QA_RUNS + pairs ? most : QA_RUNS + pairs));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * QA_NWV), 0, s, q, sel, query, scale, part); };
+    const dim3 grid((uint32_t)(most < runs ? most : runs));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * QA_NWV), 0, s, q, sel, query, scale, arrivals, part, out); };
     if (sel.list) {
         if (block == 32) { if (dtype) go(k_quant_attn<FMT, 32, 1, true>); else go(k_quant_attn<FMT, 32, 0, true>); }
         else { if (dtype) go(k_quant_attn<FMT, 64, 1, true>); else go(k_quant_attn<FMT, 64, 0, true>); }
@@ -332,11 +382,6 @@ hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint
         if (block == 32) { if (dtype) go(k_quant_attn<FMT, 32, 1, false>); else go(k_quant_attn<FMT, 32, 0, false>); }
         else { if (dtype) go(k_quant_attn<FMT, 64, 1, false>); else go(k_quant_attn<FMT, 64, 0, false>); }
     }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const dim3 cgrid(pairs, ceil_div(q.G * D, 256));
-    if (sel.list) hipLaunchKernelGGL(k_quant_combine<true>, cgrid, dim3(256), 0, s, q, sel, block, part, out);
-    else hipLaunchKernelGGL(k_quant_combine<false>, cgrid, dim3(256), 0, s, q, sel, block, part, out);
     return hipGetLastError();
 }
 

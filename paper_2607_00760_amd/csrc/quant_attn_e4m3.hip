@@ -4,10 +4,12 @@
 namespace mosaic {
 
 hipError_t launch_quant_attn_e4m3(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
-                                  float *part, float *out, hipStream_t s) {
-    return launch_quant_attn_t<QF_E4M3>(q, block, dtype, query, scale, sel, part, out, s);
+                                  void *ws, float *out, hipStream_t s) {
+    return launch_quant_attn_t<QF_E4M3>(q, block, dtype, query, scale, sel, ws, out, s);
 }
 
-size_t quant_part_bytes(int pairs) { return (size_t)(QA_RUNS + pairs) * QA_PART * sizeof(float); }
+size_t quant_attn_ws_bytes(int pairs) {
+    return (size_t)(Q_PAIRS + 1) * sizeof(uint32_t) + (size_t)(qa_runs(pairs) + pairs) * QA_PART * sizeof(float);
+}
 
 }  // namespace mosaic

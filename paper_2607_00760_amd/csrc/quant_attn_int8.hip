@@ -4,8 +4,8 @@
 namespace mosaic {
 
 hipError_t launch_quant_attn_int8(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
-                                  float *part, float *out, hipStream_t s) {
-    return launch_quant_attn_t<QF_INT8>(q, block, dtype, query, scale, sel, part, out, s);
+                                  void *ws, float *out, hipStream_t s) {
+    return launch_quant_attn_t<QF_INT8>(q, block, dtype, query, scale, sel, ws, out, s);
 }
 
 }  // namespace mosaic
