@@ -16,6 +16,7 @@ from ._lib import (OP_APPEND, OP_COMPRESS, OP_DECODE, OP_WINDOW_ROTATIONS, Mosai
 __all__ = ["Params", "MosaicCache", "QuantParams", "QuantCache", "dense_decode", "qk_norm_rope", "MosaicError", "load"]
 
 D = 128
+_I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
 
 
 @dataclass
@@ -380,20 +381,20 @@ def reorder_rotations(params: Params, k, v, ctx_lens, max_tokens: int, rot_k, ro
     return rot_k, rot_v
 
 
-def _on(device):
-    """The device made current for the calls inside (nothing to do where it is already)."""
-    import contextlib
-
+def _launch(device, call, *args):
+    """call(*args, stream), with the device current.  (The stream's handle
+    alone: a Stream object takes 3 us, as long as the launch.)"""
     import torch
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-
-def _strides3(t):
-    return (C.c_int64 * 3)(*t.stride()[:3])
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        check(call(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            check(call(*args, stream))
 
 
 def _rows(t, name, shape, dtype, device):
-    """t, checked: rows of 128 contiguous channels, 16-byte aligned, in any order."""
+    """Checks rows of 128 contiguous channels, in any order; returns t's strides."""
     import torch
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
@@ -401,11 +402,12 @@ def _rows(t, name, shape, dtype, device):
         raise ValueError(f"{name} is on {t.device}, expected {device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(-1) != 1:
+    st = t.stride()
+    if st[-1] != 1:
         raise ValueError(f"{name}: the channels of a row must be contiguous")
-    return t
+    return st
 
 
 def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, v=None,
@@ -433,51 +435,44 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
         raise ValueError(f"q has dtype {dt}, expected float16 or bfloat16")
     S, n, hq, _ = q.shape
     hkv = k.shape[2]
-    _rows(q, "q", (S, n, hq, D), dt, dev)
-    _rows(k, "k", (S, n, hkv, D), dt, dev)
-    if q_out is None:
-        q_out = torch.empty((S, n, hq, D), dtype=dt, device=dev)
-    else:
-        _rows(q_out, "q_out", (S, n, hq, D), dt, dev)
-    if k_out is None:
-        k_out = torch.empty((S, hkv, n, D), dtype=dt, device=dev)
-    else:
-        _rows(k_out, "k_out", (S, hkv, n, D), dt, dev)
     if not isinstance(positions, torch.Tensor) or positions.dtype not in (torch.int32, torch.int64):
         raise ValueError("positions must be an int32 or int64 tensor")
-    if positions.device != dev or tuple(positions.shape) != (S, n):
+    if positions.device != dev or positions.shape != (S, n):
         raise ValueError(f"positions: shape {tuple(positions.shape)} on {positions.device}, expected {(S, n)} on {dev}")
     _check_tensor(inv_freq, "inv_freq", torch.float32, dev)
     if inv_freq.dim() != 1:
         raise ValueError("inv_freq must have one dimension")
     if (q_weight is None) != (k_weight is None):
         raise ValueError("give both weights or neither")
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
+    if q_weight is not None:
+        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
             _check_tensor(w, name, dt, dev)
-            if tuple(w.shape) != (D,):
+            if w.shape != (D,):
                 raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {(D,)}")
 
-    def rows(a, b, swap):
-        ao, bo = a.stride(), b.stride()
-        order = (bo[0], bo[2], bo[1]) if swap else bo[:3]
-        return MosaicRows(a.data_ptr(), b.data_ptr(), (C.c_int64 * 3)(*ao[:3]), (C.c_int64 * 3)(*order))
-    vr = None
-    if v is not None:
-        _rows(v, "v", (S, n, hkv, D), dt, dev)
-        if v_out is None:
-            v_out = torch.empty((S, hkv, n, D), dtype=dt, device=dev)
+    def rows(x, out, name, shape, swap):
+        """x's rows and its output's ([S][Hkv][n][128] where swap is set)."""
+        a = _rows(x, name, shape, dt, dev)
+        want = (shape[0], shape[2], shape[1], D) if swap else shape
+        if out is None:
+            out = torch.empty(want, dtype=dt, device=dev)
+            b = out.stride()
         else:
-            _rows(v_out, "v_out", (S, hkv, n, D), dt, dev)
-        vr = C.byref(rows(v, v_out, True))
+            b = _rows(out, name + "_out", want, dt, dev)
+        order = _I64x3(b[0], b[2], b[1]) if swap else _I64x3(b[0], b[1], b[2])
+        return out, C.byref(MosaicRows(x.data_ptr(), out.data_ptr(), _I64x3(a[0], a[1], a[2]), order))
+    q_out, q_rows = rows(q, q_out, "q", (S, n, hq, D), False)
+    k_out, k_rows = rows(k, k_out, "k", (S, n, hkv, D), True)
+    v_rows = None
+    if v is not None:
+        v_out, v_rows = rows(v, v_out, "v", (S, n, hkv, D), True)
     elif v_out is not None:
         raise ValueError("v_out without v")
     if S and n:
-        with _on(dev):
-            check(load().mosaic_qk_norm_rope(C.byref(rows(q, q_out, False)), C.byref(rows(k, k_out, True)), vr, S, n, hq, hkv, D,
-                                             1 if dt == torch.bfloat16 else 0, _ptr(q_weight), _ptr(k_weight), float(eps),
-                                             _ptr(positions), positions.element_size(), (C.c_int64 * 2)(*positions.stride()),
-                                             _ptr(inv_freq), 2 * inv_freq.numel(), int(interleaved), _stream(dev)))
+        _launch(dev, load().mosaic_qk_norm_rope, q_rows, k_rows, v_rows, S, n, hq, hkv, D, 1 if dt == torch.bfloat16 else 0,
+                None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
+                positions.data_ptr(), positions.element_size(), _I64x2(*positions.stride()), inv_freq.data_ptr(),
+                2 * inv_freq.numel(), int(interleaved))
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 
@@ -552,6 +547,8 @@ class QuantCache:
         self._c.refused = self.refused.data_ptr()
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=self.device)
         self._cp = C.byref(self._c)
+        self._ws = (self.workspace.data_ptr(), n.value)
+        self._q_shape = (S, H * params.group_size, D)
 
     def tensors(self) -> dict:
         return {n: getattr(self, n) for n in self.TENSORS}
@@ -575,38 +572,35 @@ class QuantCache:
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("k must be a tensor [S][H][n][128]")
         shape = (S, H, k.shape[2], D)
-        _rows(k, "k", shape, self.elem, self.device)
-        _rows(v, "v", shape, self.elem, self.device)
+        ks = _rows(k, "k", shape, self.elem, self.device)
+        vs = _rows(v, "v", shape, self.elem, self.device)
         if new_lens is not None:
             _check_tensor(new_lens, "new_lens", torch.int32, self.device)
-            if tuple(new_lens.shape) != (S,):
+            if new_lens.shape != (S,):
                 raise ValueError(f"new_lens has shape {tuple(new_lens.shape)}, expected {(S,)}")
         if shape[2] == 0:
             return
-        with _on(self.device):
-            check(self.lib.mosaic_quant_append(self._cp, _ptr(k), _ptr(v), _strides3(k), _strides3(v), _ptr(new_lens), shape[2],
-                                               _stream(self.device)))
+        _launch(self.device, self.lib.mosaic_quant_append, self._cp, k.data_ptr(), v.data_ptr(), _I64x3(*ks[:3]), _I64x3(*vs[:3]),
+                None if new_lens is None else new_lens.data_ptr(), shape[2])
         self._keep = (k, v, new_lens)  # alive until the enqueued work completes
 
     def _query(self, q, out):
         import torch
-        shape = (self.num_seqs, self.params.num_kv_heads * self.params.group_size, D)
+        shape = self._q_shape
         _check_tensor(q, "q", self.elem, self.device)
-        if tuple(q.shape) != shape:
+        if q.shape != shape:
             raise ValueError(f"q shape {tuple(q.shape)} != {shape}")
         if out is None:
             return torch.empty(shape, dtype=torch.float32, device=self.device)
         _check_tensor(out, "out", torch.float32, self.device)
-        if tuple(out.shape) != shape:
+        if out.shape != shape:
             raise ValueError(f"out shape {tuple(out.shape)} != {shape}")
         return out
 
     def decode(self, q, sm_scale: float, out=None):
         """Attention over every token: q [S][H * G][128] -> fp32 [S][H * G][128]."""
         out = self._query(q, out)
-        with _on(self.device):
-            check(self.lib.mosaic_quant_decode_attention(self._cp, _ptr(q), _ptr(out), float(sm_scale), _ptr(self.workspace),
-                                                         self.workspace.numel(), _stream(self.device)))
+        _launch(self.device, self.lib.mosaic_quant_decode_attention, self._cp, q.data_ptr(), out.data_ptr(), sm_scale, *self._ws)
         return out
 
     def decode_selected(self, q, sm_scale: float, select=(1, 10), out=None, blocks=None):
@@ -620,8 +614,6 @@ class QuantCache:
             _check_tensor(blocks, "blocks", torch.int32, self.device)
             if blocks.shape != self.k_scale.shape:
                 raise ValueError(f"blocks shape {tuple(blocks.shape)} != {tuple(self.k_scale.shape)}")
-        with _on(self.device):
-            check(self.lib.mosaic_quant_select_attention(self._cp, _ptr(q), _ptr(out), float(sm_scale), int(select[0]), int(select[1]),
-                                                         _ptr(blocks), _ptr(self.workspace), self.workspace.numel(),
-                                                         _stream(self.device)))
+        _launch(self.device, self.lib.mosaic_quant_select_attention, self._cp, q.data_ptr(), out.data_ptr(), sm_scale, int(select[0]),
+                int(select[1]), None if blocks is None else blocks.data_ptr(), *self._ws)
         return out
