@@ -32,7 +32,7 @@ struct QNew {                                              // tokens to append, 
 };
 
 // How a launch of about `slots` workgroups shares the units of all pairs: runs
-// of c units, c a multiple of cmin, that do not cross pairs.  The lengths are
+// of c >= cmin units, c a multiple of step, that do not cross pairs.  The lengths are
 // read on the device, so a captured launch follows them; runs are equal
 // however ragged the batch, and there are at most slots + pairs of them.
 struct QPlan {
@@ -43,7 +43,7 @@ struct QPlan {
 
 // units(L): units of a pair of L tokens; least: runs of a pair at least.
 template <typename U>
-__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int least, U units, int w) {
+__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int step, int least, U units, int w) {
     const int lane = threadIdx.x & 63;
     uint32_t total = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
@@ -52,7 +52,7 @@ __device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, in
     }
     total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(total), 63) * (uint32_t)q.H;
     const uint32_t c0 = (total + (uint32_t)slots - 1u) / (uint32_t)slots;
-    const int c = max(cmin, (int)((c0 + (uint32_t)cmin - 1u) / (uint32_t)cmin) * cmin);
+    const int c = max(cmin, (int)((c0 + (uint32_t)step - 1u) / (uint32_t)step) * step);
     QPlan p{};
     p.c = c;
     uint32_t base = 0;

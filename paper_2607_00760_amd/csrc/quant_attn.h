@@ -29,6 +29,9 @@ constexpr int QA_NWV = 4;                                  // waves of a workgro
 // Runs of a launch: with up to 256 pairs they and the pairs' rounding fill the
 // 512 workgroups that the chip holds once; more pairs take several rounds anyway.
 __host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256 ? 512 - pairs : 1024; }
+// Blocks of a run at least: two steps a wave.  1 x 4117 tokens, 8 kv heads: 4
+// blocks 11.5 us, 8 9.6, 16 11.7 (a step costs less than joining twice the runs).
+constexpr int QA_LEAST = 2 * QA_NWV;
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: max, sum, accumulators
 
@@ -126,7 +129,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     __shared__ __align__(16) float mrg[QA_NWV][16][D + 2];
     __shared__ int last;
     auto units = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
-    const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_NWV, 1, units, blockIdx.x);
+    const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_LEAST, QA_NWV, 1, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -134,18 +137,38 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     const int b0 = pl.i * pl.c, b1 = min(units(pl.L), b0 + pl.c), rest = pl.i == pl.ns - 1 ? pl.L % B : 0;
     const int head = min(l16 & 7, q.G - 1);                // (columns past the group repeat its last head)
     const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
+    const int32_t *list = SEL ? sel.list + (uint64_t)p * q.N : nullptr;
+    const uint64_t pb = (uint64_t)p * q.N;
+    auto load = [&](int t, QStage<FMT, B> &st) {
+        const uint64_t blk = pb + (uint32_t)(SEL ? list[t] : t);
+        const uint8_t *kp = q.k + blk * (B * D), *vp = q.v + blk * (B * D);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                st.k[n][j] = *(const uint4 *)(kp + (TPQ * (l16 >> 2) + 4 * n + (l16 & 3)) * D + 64 * j + 16 * q4);
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) __builtin_memcpy(st.v[ct], __builtin_assume_aligned(vp + (16 * ct + l16) * B + TPQ * q4, TPQ), TPQ);
+        st.ks = q.ks[blk];
+        st.vs = q.vs[blk];
+    };
+    QStage<FMT, B> st0, st1;
+    int t = b0 + wave;
     // q operand: column l16 is head l16 % 8, inner index (j, half, q4, i) channel 64 j + 16 q4 + 8 half + i
     dhf8 qb[4];
     float zs;                                              // softmax scale in powers of two, and q's
     {
+        uint16_t w[4][8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) __builtin_memcpy(w[e], __builtin_assume_aligned(qp + 64 * (e >> 1) + 16 * q4 + 8 * (e & 1), 16), 16);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t < b1) load(t, st0);                          // on its way while q is looked at
+        __builtin_amdgcn_sched_barrier(0);
         float x[4][8], a = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint16_t w[8];
-            __builtin_memcpy(w, qp + 64 * (e >> 1) + 16 * q4 + 8 * (e & 1), 16);
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { x[e][i] = h2f(w[i], DT); a = fmaxf(a, fabsf(x[e][i])); }
-        }
+            for (int i = 0; i < 8; ++i) { x[e][i] = h2f(w[e][i], DT); a = fmaxf(a, fabsf(x[e][i])); }
         float down = 1.0f;
         zs = scale * 1.44269504088896340736f;
         if (DT) {                                          // largest magnitude in [1, 2), what falls below 2^-24 of it is lost
@@ -210,21 +233,6 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             scale_acc(f);
         }
     };
-    const int32_t *list = SEL ? sel.list + (uint64_t)p * q.N : nullptr;
-    const uint64_t pb = (uint64_t)p * q.N;
-    auto load = [&](int t, QStage<FMT, B> &st) {
-        const uint64_t blk = pb + (uint32_t)(SEL ? list[t] : t);
-        const uint8_t *kp = q.k + blk * (B * D), *vp = q.v + blk * (B * D);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                st.k[n][j] = *(const uint4 *)(kp + (TPQ * (l16 >> 2) + 4 * n + (l16 & 3)) * D + 64 * j + 16 * q4);
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) __builtin_memcpy(st.v[ct], __builtin_assume_aligned(vp + (16 * ct + l16) * B + TPQ * q4, TPQ), TPQ);
-        st.ks = q.ks[blk];
-        st.vs = q.vs[blk];
-    };
     auto consume = [&](const QStage<FMT, B> &st) {
         float z[NT][4];
 #pragma unroll
@@ -253,9 +261,6 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, codes_f16<FMT>(st.v[ct][2 * s], st.v[ct][2 * s + 1]), acc[ct]);
         }
     };
-    QStage<FMT, B> st0, st1;
-    int t = b0 + wave;
-    if (t < b1) load(t, st0);
     while (t < b1) {                                       // (two steps a turn: no copies that would wait on the loads)
         load(t + QA_NWV < b1 ? t + QA_NWV : t, st1);       // (the last step loads itself again)
         __builtin_amdgcn_sched_barrier(0);
@@ -372,7 +377,7 @@ hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint
     uint32_t *arrivals = (uint32_t *)ws;
     float *part = (float *)(arrivals + Q_PAIRS + 1);
     const int blocks = sel.list ? q_want(q.N, sel.num, sel.den) : q.N;
-    const long long most = (long long)pairs * ceil_div(blocks, QA_NWV);
+    const long long most = (long long)pairs * ceil_div(blocks, QA_LEAST);
     const dim3 grid((uint32_t)(most < runs ? most : runs));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * QA_NWV), 0, s, q, sel, query, scale, arrivals, part, out); };
     if (sel.list) {

@@ -43,7 +43,7 @@ __device__ __forceinline__ i32x4 pack_signed(const float (&x)[16], bool upper) {
 // looked at.
 template <int DT>
 __global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores) {
-    const QPlan pl = q_plan(q, QS_RUNS, 1, 0, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
+    const QPlan pl = q_plan(q, QS_RUNS, 1, 1, 0, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
     if (!pl.live) return;
     const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int p = pl.s * q.H + pl.h, nb = pl.L / block;
