@@ -502,6 +502,7 @@ typedef struct {
     void *k_tail;                      /* [S][H][B][128] of the dtype, 16-byte aligned */
     void *v_tail;                      /* [S][H][128][B] of the dtype, 16-byte aligned */
     int32_t *lens;                     /* [S][H] tokens held (a sequence's entries are equal) */
+    int32_t *arrivals;                 /* [S][H][32] the library's own; zero before the first append */
     int32_t *refused;                  /* [S] appends that a sequence had no room for */
 } mosaic_quant_cache;
 

@@ -545,6 +545,8 @@ class QuantCache:
         #: appends that each sequence had no room for (it took none of their tokens)
         self.refused = torch.zeros(S, dtype=torch.int32, device=self.device)
         self._c.refused = self.refused.data_ptr()
+        self._arrivals = torch.zeros((S, H, 32), dtype=torch.int32, device=self.device)
+        self._c.arrivals = self._arrivals.data_ptr()
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=self.device)
         self._cp = C.byref(self._c)
         self._ws = (self.workspace.data_ptr(), n.value)

@@ -61,7 +61,8 @@ class MosaicRows(C.Structure):
 class MosaicQuantCache(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("num_seqs", "num_kv_heads", "group_size", "head_dim", "dtype", "format", "block_len",
                                          "max_blocks")] + [
-        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens", "refused")]
+        (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens", "arrivals",
+                                  "refused")]
 
 
 class MosaicStats(C.Structure):

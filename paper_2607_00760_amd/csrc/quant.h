@@ -10,6 +10,8 @@ constexpr float QLEAST = 7.888609052210118e-31f;          // 2^-100: magnitudes 
 constexpr int QF_E4M3 = 0, QF_INT8 = 1;
 __host__ __device__ constexpr float q_top(int fmt) { return fmt == QF_INT8 ? 127.0f : 448.0f; }
 
+constexpr int Q_ARRIVALS = 32;                             // a counter has a line of its own
+
 // The cache's tensors (mosaic_quant_cache), passed by value.
 struct QCache {
     int S, H, G, N;                                        // sequences, kv heads, group, blocks of a pair at most
@@ -19,6 +21,7 @@ struct QCache {
     int8_t *bounds;                                        // [S][H][N][2][D]: upper, lower
     uint16_t *kt, *vt;                                     // unfinished block [S][H][B][D] and [S][H][D][B]
     int32_t *lens;                                         // [S][H]: a pair's workgroups need no other pair's
+    int32_t *arrivals;                                     // [S][H][Q_ARRIVALS], the first of each used; zero between appends
     int32_t *refused;                                      // [S]: appends that a sequence had no room for
     // a pair's length; one that no append can have left reads as the nearest that can
     __device__ __forceinline__ int len(long long p) const { return min(max(lens[p], 0), cap); }

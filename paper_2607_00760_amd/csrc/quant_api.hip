@@ -50,14 +50,15 @@ mosaic_status quant_arrays(const mosaic_quant_cache *c, QCache &q) {
     const mosaic_status st = quant_shape(c);
     if (st != MOSAIC_OK) return st;
     if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->bound_scale || !c->bounds || !c->k_tail || !c->v_tail || !c->lens ||
-        !c->refused)
+        !c->arrivals || !c->refused)
         return fail(MOSAIC_ERR_INVALID, "NULL array in the cache");
     if (off16(c->k) || off16(c->v) || off16(c->bounds) || off16(c->k_tail) || off16(c->v_tail))
         return fail(MOSAIC_ERR_INVALID, "codes, bounds and tails must be 16-byte aligned");
-    if (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->bound_scale | (uintptr_t)c->lens | (uintptr_t)c->refused) % 4)
+    if (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale | (uintptr_t)c->bound_scale | (uintptr_t)c->lens | (uintptr_t)c->arrivals |
+         (uintptr_t)c->refused) % 4)
         return fail(MOSAIC_ERR_INVALID, "scales and lengths must be 4-byte aligned");
     q = QCache{c->num_seqs, c->num_kv_heads, c->group_size, c->max_blocks, c->max_blocks * c->block_len, (uint8_t *)c->k, (uint8_t *)c->v, c->k_scale, c->v_scale,
-               c->bound_scale, c->bounds, (uint16_t *)c->k_tail, (uint16_t *)c->v_tail, c->lens, c->refused};
+               c->bound_scale, c->bounds, (uint16_t *)c->k_tail, (uint16_t *)c->v_tail, c->lens, c->arrivals, c->refused};
     return MOSAIC_OK;
 }
 

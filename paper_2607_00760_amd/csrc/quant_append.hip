@@ -20,6 +20,8 @@ namespace mosaic {
 
 namespace {
 
+constexpr int QN_ARRIVE = 32;
+
 // bytes e of four words: the columns of a 4 x 4 byte matrix
 __device__ __forceinline__ void turn4(const uint32_t (&r)[4], uint32_t (&c)[4]) {
     const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
@@ -30,31 +32,36 @@ __device__ __forceinline__ void turn4(const uint32_t (&r)[4], uint32_t (&c)[4]) 
     c[3] = __builtin_amdgcn_perm(e, b, 0x07060302u);
 }
 
-// codes of four values already in units of the scale, one byte each
+// Codes of four values already in units of the scale, one byte each.  No value
+// of a block is past the largest code by more than a rounding, so nothing is
+// clamped; integers come out of the lowest bits of 1.5 * 2^23 + y.
 template <int FMT> __device__ __forceinline__ uint32_t codes4(const float (&y)[4]) {
     if (FMT == QF_E4M3) {
-        float z[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = __builtin_amdgcn_fmed3f(y[i], -448.0f, 448.0f);
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], w, true);
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
     }
-    uint32_t w = 0;
+    uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(y[i]), -127.0f, 127.0f) & 0xffu) << (8 * i);
-    return w;
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(y[i] + 12582912.0f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u), __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), 0x05040100u);
 }
 
-// grid (blocks that the call may complete, pairs).  solo: the grid has one
-// block, so its workgroup is the only one that needs the length and writes it.
+// grid (blocks that the call may complete, pairs).  The last of a
+// pair's workgroups to have read the length writes the new one; grids of more
+// than QN_ARRIVE blocks leave that to a launch of its own (4 us): an arrival at
+// one address takes 12 ns, and 1025 a pair of 32 took the prefill of 4 x 32785
+// tokens from 160 to 176 us (and to 388 with the pairs' counters in one line).
 template <int FMT, int B, int DT>
-__global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw, int solo) {
+__global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw) {
     constexpr int HW = 4 * B / 64;                             // waves of a half
     __shared__ float red[2 * HW];
     __shared__ float bnd[HW][16][16];                          // [wave][8 upper, 8 lower of 8 channels][channel group]
     const int p = blockIdx.y, j = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = p / q.H, h = p - s * q.H;
-    const int vals = tid >= 4 * B, t4 = (tid & (4 * B - 1)) >> 4, pc = tid & 15;
+    // 4 tokens x 8 channels of a thread: rows side by side for the keys, whose
+    // codes lie by token, token groups side by side for the values
+    const int vals = tid >= 4 * B, ht = tid & (4 * B - 1);
+    const int t4 = vals ? ht & (B / 4 - 1) : ht >> 4, pc = vals ? ht / (B / 4) : ht & 15;
     const int L = q.len(p);
     int n = nw.counts ? nw.counts[s] : nw.max_new;
     n = min(max(n, 0), nw.max_new);
@@ -64,7 +71,18 @@ __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw, int s
         return;
     }
     const int f = L % B, first = L / B, done = (f + n) / B;
-    if (j > 0 && j >= done) return;
+    int32_t *arrivals = q.arrivals + (uint64_t)p * Q_ARRIVALS;
+    auto arrive = [&] {
+        if (gridDim.x > QN_ARRIVE) return;
+        __syncthreads();                                       // every thread has read the length
+        if (tid != 0) return;
+        if (gridDim.x > 1) {
+            if (__hip_atomic_fetch_add(arrivals, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (int)gridDim.x - 1) return;
+            __hip_atomic_store(arrivals, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        q.lens[p] = L + n;
+    };
+    if (j > 0 && j >= done) { arrive(); return; }
     const uint16_t *src = vals ? nw.v + s * nw.v_seq + h * nw.v_head : nw.k + s * nw.k_seq + h * nw.k_head;
     const int64_t tok = vals ? nw.v_tok : nw.k_tok;
     uint16_t *kt = q.kt + (uint64_t)p * B * D, *vt = q.vt + (uint64_t)p * B * D;
@@ -152,7 +170,7 @@ __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw, int s
             }
         }
     }
-    if (j > 0) return;
+    if (j > 0) { arrive(); return; }
     // the tokens that no block holds yet: from here on the tail's old rows have
     // been read (the barrier above), or stay where they are
     const int rest = f + n - done * B, t0 = done ? 0 : f;
@@ -166,13 +184,9 @@ __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw, int s
 #pragma unroll
         for (int e = 0; e < 8; ++e) vt[(8 * g + e) * B + t] = (uint16_t)((e & 1) ? (w[e >> 1] >> 16) : w[e >> 1]);
     }
-    if (solo) {
-        __syncthreads();                                       // every thread has read the length
-        if (tid == 0) q.lens[p] = L + n;
-    }
+    arrive();
 }
 
-// the lengths after a call whose pairs had several workgroups
 __global__ void __launch_bounds__(256) k_quant_lens(QCache q, QNew nw) {
     const int p = blockIdx.x * 256 + threadIdx.x;
     if (p >= q.S * q.H) return;
@@ -183,10 +197,9 @@ __global__ void __launch_bounds__(256) k_quant_lens(QCache q, QNew nw) {
 }  // namespace
 
 hipError_t launch_quant_append(const QCache &q, int fmt, int block, int dtype, const QNew &n, hipStream_t s) {
-    const int most = (block - 1 + n.max_new) / block, solo = most <= 1;
-    const int pairs = q.S * q.H;
+    const int most = (block - 1 + n.max_new) / block, pairs = q.S * q.H;
     const dim3 grid(most < 1 ? 1 : most, pairs);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(8 * block), 0, s, q, n, solo); };
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(8 * block), 0, s, q, n); };
     auto by_type = [&](auto f, auto b) {
         constexpr int F = decltype(f)::value, B = decltype(b)::value;
         if (dtype) go(k_quant_append<F, B, 1>); else go(k_quant_append<F, B, 0>);
@@ -199,8 +212,8 @@ hipError_t launch_quant_append(const QCache &q, int fmt, int block, int dtype, c
         if (block == 32) by_type(integral_constant<int, QF_E4M3>{}, integral_constant<int, 32>{});
         else by_type(integral_constant<int, QF_E4M3>{}, integral_constant<int, 64>{});
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || solo) return e;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || most <= QN_ARRIVE) return e;
     hipLaunchKernelGGL(k_quant_lens, dim3(ceil_div(pairs, 256)), dim3(256), 0, s, q, n);
     return hipGetLastError();
 }

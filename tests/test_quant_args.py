@@ -14,7 +14,7 @@ from paper_2607_00760_amd import _lib  # noqa: E402
 
 OK, INVALID, UNSUPPORTED, CAPACITY, HIP = 0, -1, -2, -3, -5
 FAKE = 0x100000
-ARRAYS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens", "refused")
+ARRAYS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens", "arrivals", "refused")
 
 
 @pytest.fixture(scope="module")
