@@ -48,11 +48,10 @@ struct QPlan {
 template <typename U>
 __device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int step, int least, U units, int w) {
     const int lane = threadIdx.x & 63;
-    uint32_t total = 0;
-    for (int s0 = 0; s0 < q.S; s0 += 64) {
-        const int s = s0 + lane;
-        total += s < q.S ? (uint32_t)units(q.len((long long)s * q.H)) : 0u;
-    }
+    auto length = [&](int s) { return s < q.S ? q.len((long long)s * q.H) : 0; };
+    const int L0 = length(lane);
+    uint32_t total = lane < q.S ? (uint32_t)units(L0) : 0u;
+    for (int s = lane + 64; s < q.S; s += 64) total += (uint32_t)units(length(s));
     total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(total), 63) * (uint32_t)q.H;
     const uint32_t c0 = (total + (uint32_t)slots - 1u) / (uint32_t)slots;
     const int c = max(cmin, (int)((c0 + (uint32_t)step - 1u) / (uint32_t)step) * step);
@@ -60,8 +59,7 @@ __device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, in
     p.c = c;
     uint32_t base = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
-        const int s = s0 + lane;
-        const int L = s < q.S ? q.len((long long)s * q.H) : 0;
+        const int s = s0 + lane, L = s0 ? length(s) : L0;
         const int ns = s < q.S ? max(least, (units(L) + c - 1) / c) : 0;
         const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
         const uint64_t hit = __ballot(base + inc > (uint32_t)w);       // the first sequence whose runs end past w

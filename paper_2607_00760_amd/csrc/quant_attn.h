@@ -33,7 +33,7 @@ __host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256
 // blocks 11.5 us, 8 9.6, 16 11.7 (a step costs less than joining twice the runs).
 constexpr int QA_LEAST = 2 * QA_NWV;
 constexpr int QA_HEADS = 8;
-constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: max, sum, accumulators
+constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and accumulators of the heads
 
 // 8 codes as fp16
 template <int FMT> __device__ __forceinline__ dhf8 codes_f16(uint32_t a, uint32_t b) {
@@ -67,7 +67,6 @@ __device__ __forceinline__ float joined(float a, float s) { return s > 0.0f ? a 
 
 // partials, past the XCD's L2
 __device__ __forceinline__ void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float2 get2(const float *p) {
     return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
@@ -81,29 +80,36 @@ __device__ __forceinline__ void join_runs(const float *part, int ns, int G, floa
     const int share = tid / cols, col = tid - share * cols, h = col >> 5;
     float M = -INFINITY, S = 0.0f;
     float4 A = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto add = [&](float m, float l, float4 a) {
-        if (m == -INFINITY) return;
-        const float mn = fmaxf(M, m);
-        const float x = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mn), y = __builtin_amdgcn_exp2f(m - mn);
-        A = make_float4(A.x * x + a.x * y, A.y * x + a.y * y, A.z * x + a.z * y, A.w * x + a.w * y);
-        S = S * x + l * y;
-        M = mn;
-    };
     if (share < np)
         for (int r0 = share; r0 < ns; r0 += CB * np) {
-            float m[CB], l[CB];
-            float4 a[CB];
+            float2 ml[CB], a[CB][2];
 #pragma unroll
             for (int e = 0; e < CB; ++e) {
                 const float *ps = part + (uint64_t)min(r0 + e * np, ns - 1) * QA_PART;
-                m[e] = get(ps + h);
-                l[e] = get(ps + QA_HEADS + h);
-                const float2 lo = get2(ps + 2 * QA_HEADS + 4 * col), hi = get2(ps + 2 * QA_HEADS + 4 * col + 2);
-                a[e] = make_float4(lo.x, lo.y, hi.x, hi.y);
+                ml[e] = get2(ps + 2 * h);
+                a[e][0] = get2(ps + 2 * QA_HEADS + 4 * col);
+                a[e][1] = get2(ps + 2 * QA_HEADS + 4 * col + 2);
             }
+            float mn = M;
 #pragma unroll
-            for (int e = 0; e < CB; ++e)
-                if (r0 + e * np < ns) add(m[e], l[e], a[e]);
+            for (int e = 0; e < CB; ++e) {
+                if (r0 + e * np >= ns) ml[e] = make_float2(-INFINITY, 0.0f);
+                mn = fmaxf(mn, ml[e].x);
+            }
+            const float mb = mn == -INFINITY ? 0.0f : mn, x = __builtin_amdgcn_exp2f(M - mb);
+            A = make_float4(A.x * x, A.y * x, A.z * x, A.w * x);
+            S *= x;
+            M = mn;
+#pragma unroll
+            for (int e = 0; e < CB; ++e) {
+                if (r0 + e * np >= ns) continue;
+                const float y = __builtin_amdgcn_exp2f(ml[e].x - mb);
+                A.x = fmaf(a[e][0].x, y, A.x);
+                A.y = fmaf(a[e][0].y, y, A.y);
+                A.z = fmaf(a[e][1].x, y, A.z);
+                A.w = fmaf(a[e][1].y, y, A.w);
+                S = fmaf(ml[e].y, y, S);
+            }
         }
     float *x = lds + 8 * tid;
     if (share > 0 && share < np) {
@@ -114,8 +120,13 @@ __device__ __forceinline__ void join_runs(const float *part, int ns, int G, floa
     __syncthreads();
     if (share > 0) return;
     for (int e = 1; e < np; ++e) {
-        const float *y = lds + 8 * (tid + e * cols);
-        add(y[4], y[5], *(const float4 *)y);
+        const float *o = lds + 8 * (tid + e * cols);
+        const float4 a = *(const float4 *)o;
+        const float mn = fmaxf(M, o[4]), mb = mn == -INFINITY ? 0.0f : mn;
+        const float x = __builtin_amdgcn_exp2f(M - mb), y = __builtin_amdgcn_exp2f(o[4] - mb);
+        A = make_float4(A.x * x + a.x * y, A.y * x + a.y * y, A.z * x + a.z * y, A.w * x + a.w * y);
+        S = S * x + o[5] * y;
+        M = mn;
     }
     *(float4 *)(out + 4 * col) = make_float4(joined(A.x, S), joined(A.y, S), joined(A.z, S), joined(A.w, S));
 }
@@ -128,19 +139,21 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     constexpr float PS = 16384.0f;                         // small weights stay in fp16's normal range
     __shared__ __align__(16) float mrg[QA_NWV][16][D + 2];
     __shared__ int last;
-    auto units = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
+    auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
+    auto units = [&](int L) { return blocks(L) + (L % B != 0); };        // the unfinished block is a pair's last unit
     const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_LEAST, QA_NWV, 1, units, blockIdx.x);
     if (!pl.live) return;
-    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q4 = lane >> 4;
+    const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int p = pl.s * q.H + pl.h;
-    const int b0 = pl.i * pl.c, b1 = min(units(pl.L), b0 + pl.c), rest = pl.i == pl.ns - 1 ? pl.L % B : 0;
+    const int b0 = pl.i * pl.c, b1 = min(blocks(pl.L), b0 + pl.c), rest = min(units(pl.L), b0 + pl.c) > b1 ? pl.L % B : 0;
+    const int l16 = tid & 15, q4 = (tid & 63) >> 4;
     const int head = min(l16 & 7, q.G - 1);                // (columns past the group repeat its last head)
     const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
     const int32_t *list = SEL ? sel.list + (uint64_t)p * q.N : nullptr;
     const uint64_t pb = (uint64_t)p * q.N;
-    auto load = [&](int t, QStage<FMT, B> &st) {
-        const uint64_t blk = pb + (uint32_t)(SEL ? list[t] : t);
+    auto load = [&](int id, QStage<FMT, B> &st) {
+        const uint64_t blk = pb + (uint32_t)id;
         const uint8_t *kp = q.k + blk * (B * D), *vp = q.v + blk * (B * D);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -154,6 +167,11 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     };
     QStage<FMT, B> st0, st1;
     int t = b0 + wave;
+    // the wave's blocks of this step and the next (a selection's are read one
+    // step ahead of their loads; past the run's end the last again)
+    auto block_at = [&](int u) { return SEL ? list[min(u, b1 - 1)] : min(u, b1 - 1); };
+    int id0 = 0, id1 = 0;
+    if (t < b1) { id0 = block_at(t); id1 = block_at(t + QA_NWV); }
     // q operand: column l16 is head l16 % 8, inner index (j, half, q4, i) channel 64 j + 16 q4 + 8 half + i
     dhf8 qb[4];
     float zs;                                              // softmax scale in powers of two, and q's
@@ -162,7 +180,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
 #pragma unroll
         for (int e = 0; e < 4; ++e) __builtin_memcpy(w[e], __builtin_assume_aligned(qp + 64 * (e >> 1) + 16 * q4 + 8 * (e & 1), 16), 16);
         __builtin_amdgcn_sched_barrier(0);
-        if (t < b1) load(t, st0);                          // on its way while q is looked at
+        if (t < b1) load(id0, st0);                        // on its way while q is looked at
         __builtin_amdgcn_sched_barrier(0);
         float x[4][8], a = 0.0f;
 #pragma unroll
@@ -187,18 +205,12 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     df4 acc[8];                                            // [channel tile][row 4 q4 + r]
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) acc[ct] = df4{0.0f, 0.0f, 0.0f, 0.0f};
-    auto scale_acc = [&](const float (&f)[4]) {
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[ct][r] *= f[r];
-    };
     // the softmax's step over logits z, to weights in units that make acc's
     auto weigh = [&](float (&z)[NT][4], float vs) {
+        float grow = 1.0f;                                 // of acc's unit
         if (vs > ref) {
-            const float up = __uint_as_float((__float_as_uint(vs) & 0x7f800000u) + 0x00800000u), f = ref / up;
-            const float ff[4] = {f, f, f, f};
-            scale_acc(ff);
+            const float up = __uint_as_float((__float_as_uint(vs) & 0x7f800000u) + 0x00800000u);
+            grow = ref / up;
             ref = up;
         }
         float cm = -INFINITY;
@@ -222,15 +234,18 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             }
         l_run = fmaf(l_run, alpha, ls);
         m_run = mn;
-        if (!__all(alpha == 1.0f)) {                       // some head's running maximum moved
+        if (grow != 1.0f || !__all(alpha == 1.0f)) {       // the unit or some head's running maximum moved
             float f[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {                  // alpha of head (4 q4 + r) % 8
                 const float a0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), r));
                 const float a1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), 4 + r));
-                f[r] = (q4 & 1) ? a1 : a0;
+                f[r] = ((q4 & 1) ? a1 : a0) * grow;
             }
-            scale_acc(f);
+#pragma unroll
+            for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[ct][r] *= f[r];
         }
     };
     auto consume = [&](const QStage<FMT, B> &st) {
@@ -262,12 +277,14 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         }
     };
     while (t < b1) {                                       // (two steps a turn: no copies that would wait on the loads)
-        load(t + QA_NWV < b1 ? t + QA_NWV : t, st1);       // (the last step loads itself again)
+        load(id1, st1);
+        id0 = block_at(t + 2 * QA_NWV);
         __builtin_amdgcn_sched_barrier(0);
         consume(st0);
         t += QA_NWV;
         if (t >= b1) break;
-        load(t + QA_NWV < b1 ? t + QA_NWV : t, st0);
+        load(id0, st0);
+        id1 = block_at(t + 2 * QA_NWV);
         __builtin_amdgcn_sched_barrier(0);
         consume(st1);
         t += QA_NWV;
@@ -275,6 +292,10 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     if (rest && wave == ((b1 - b0) & (QA_NWV - 1))) {      // the unfinished block, in 16 bits
         using M8 = typename DM::v8;
         using E = typename DM::el;
+        int at = tid;                                      // (worked out again: nothing of it lives through the loop)
+        asm volatile("" : "+v"(at));
+        const int l16 = at & 15, q4 = (at & 63) >> 4;
+        const uint16_t *qp = query + ((uint64_t)p * q.G + min(l16 & 7, q.G - 1)) * D;
         const uint16_t *kp = q.kt + (uint64_t)p * B * D, *vp = q.vt + (uint64_t)p * B * D;
         M8 qd[4];
 #pragma unroll
@@ -323,11 +344,15 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     // join the waves
     l_run = rows_all(l_run, [](float a, float b) { return a + b; });
     const float back = ref * (1.0f / PS);
-    if (lane < 16) { mrg[wave][l16][0] = m_run; mrg[wave][l16][1] = l_run; }
+    int lane = tid;
+    asm volatile("" : "+v"(lane));
+    lane &= 63;
+    const int row = lane >> 4, col = lane & 15;   // (worked out again, as above)
+    if (lane < 16) { mrg[wave][col][0] = m_run; mrg[wave][col][1] = l_run; }
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) mrg[wave][4 * q4 + r][2 + 16 * ct + l16] = acc[ct][r] * back;
+        for (int r = 0; r < 4; ++r) mrg[wave][4 * row + r][2 + 16 * ct + col] = acc[ct][r] * back;
     __syncthreads();
     float *out = outp + (uint64_t)p * q.G * D;
     // partials of a pair's runs are consecutive: run 0's is this workgroup's less pl.i
@@ -348,7 +373,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             out[i] = joined(A, S);
         } else {
             put(mine + 2 * QA_HEADS + i, A);
-            if (c == 0) { put(mine + h, M); put(mine + QA_HEADS + h, S); }
+            if (c == 0) { put(mine + 2 * h, M); put(mine + 2 * h + 1, S); }
         }
     }
     if (pl.ns == 1) return;
@@ -376,8 +401,8 @@ hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint
     const int pairs = q.S * q.H, runs = qa_runs(pairs) + pairs;
     uint32_t *arrivals = (uint32_t *)ws;
     float *part = (float *)(arrivals + Q_PAIRS + 1);
-    const int blocks = sel.list ? q_want(q.N, sel.num, sel.den) : q.N;
-    const long long most = (long long)pairs * ceil_div(blocks, QA_LEAST);
+    const int units = (sel.list ? q_want(q.N, sel.num, sel.den) : q.N) + 1;
+    const long long most = (long long)pairs * ceil_div(units, QA_LEAST);
     const dim3 grid((uint32_t)(most < runs ? most : runs));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * QA_NWV), 0, s, q, sel, query, scale, arrivals, part, out); };
     if (sel.list) {

@@ -42,7 +42,7 @@ __device__ __forceinline__ i32x4 pack_signed(const float (&x)[16], bool upper) {
 // QS_AHEAD steps of 16 blocks in flight; the first are out before the query is
 // looked at.
 template <int DT>
-__global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores) {
+__global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores, int32_t *list) {
     const QPlan pl = q_plan(q, QS_RUNS, 1, 1, 0, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
     if (!pl.live) return;
     const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -68,6 +68,11 @@ __global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const 
         }
     };
     load();
+    {                                                      // the list's places, -1 until the selection takes them
+        int32_t *lp = list + (uint64_t)p * q.N;
+        const int e1 = pl.i == pl.ns - 1 ? q.N : b1;
+        for (int e = pl.i * pl.c * QS_UNIT + threadIdx.x; e < e1; e += 256) lp[e] = -1;
+    }
     const int head = min(l16, q.G - 1);                    // columns past the group repeat its last head
     const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
     float x[2][16];
@@ -121,7 +126,7 @@ template <int KPT>
 __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int num, int den, const float *scores, int32_t *list) {
     constexpr int NW = 16, NT = 64 * NW, BINS = 2048, BPT = BINS / NT, FEW = 64;
     __shared__ uint32_t hist[2][BINS];
-    __shared__ uint32_t mm[2 * NW], pk[NW], pub[3], sc[2][NW], few[FEW], nfew;
+    __shared__ uint32_t mm[2 * NW], pk[NW], pub[3], sc[2][NW], few[FEW], cmp[FEW], nfew;
     const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int nb = q.len(p) / block, want = q_want(nb, num, den);
     const float *src = scores + (uint64_t)p * q_score_stride(q.N);
@@ -143,8 +148,11 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
     }
     for (int i = tid; i < BINS; i += NT) hist[0][i] = 0u;
     if (tid == 0) nfew = 0u;
-    for (int i = want + tid; i < q.N; i += NT) dst[i] = -1;
-    if (want == 0) return;
+    if (tid < FEW) cmp[tid] = 0u;
+    if (want == 0) {                                       // (no scores were made)
+        for (int i = tid; i < q.N; i += NT) dst[i] = -1;
+        return;
+    }
     auto each = [&](auto f) {
         if (KPT) {
 #pragma unroll
@@ -190,13 +198,16 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
             const int n = (int)pub[2];
             each([&](int, uint32_t k) { if (k >= base && k - base <= span) few[atomicAdd(&nfew, 1u)] = k; });
             lds_barrier();
+            // a wave compares every candidate, a lane each, with its share of them
             const uint32_t k = lane < n ? few[lane] : 0u;
-            uint32_t gt = 0u, ge = 0u;
-            for (int e = 0; e < n; ++e) {
+            uint32_t c = 0u;                               // candidates above, and from bit 16 equal ones
+            for (int e = wv; e < n; e += NW) {
                 const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)k, e);
-                gt += o > k ? 1u : 0u;
-                ge += o >= k ? 1u : 0u;
+                c += o > k ? 1u : (o == k ? 0x10000u : 0u);
             }
+            if (c) atomicAdd(&cmp[lane], c);
+            lds_barrier();
+            const uint32_t gt = cmp[lane] & 0xffffu, ge = gt + (cmp[lane] >> 16);
             const int l = (int)__builtin_ctzll(__ballot(lane < n && gt < rem && ge >= rem));   // (rem of the n are needed: never empty)
             base = (uint32_t)__builtin_amdgcn_readlane((int)k, l);
             rem -= (uint32_t)__builtin_amdgcn_readlane((int)gt, l);
@@ -222,8 +233,8 @@ hipError_t launch_quant_select(const QCache &q, int block, int dtype, const uint
     const int pairs = q.S * q.H;
     const long long most = (long long)pairs * ceil_div(q.N, QS_UNIT);
     const dim3 grid((uint32_t)(most < QS_RUNS + pairs ? most : QS_RUNS + pairs));
-    if (dtype) hipLaunchKernelGGL(k_quant_score<1>, grid, dim3(256), 0, s, q, block, query, scores);
-    else hipLaunchKernelGGL(k_quant_score<0>, grid, dim3(256), 0, s, q, block, query, scores);
+    if (dtype) hipLaunchKernelGGL(k_quant_score<1>, grid, dim3(256), 0, s, q, block, query, scores, list);
+    else hipLaunchKernelGGL(k_quant_score<0>, grid, dim3(256), 0, s, q, block, query, scores, list);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pairs), dim3(1024), 0, s, q, block, num, den, scores, list); };
