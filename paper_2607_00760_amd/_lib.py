@@ -129,11 +129,10 @@ def bind_signatures(L: C.CDLL) -> C.CDLL:
     L.mosaic_last_error.argtypes = []
     L.mosaic_last_error.restype = C.c_char_p
     if hasattr(L, "mosaic_quant_append"):                   # (a library of the cache's host layer alone has the rest)
-        qc, st3 = C.POINTER(MosaicQuantCache), C.POINTER(C.c_int64)
-        rows = C.POINTER(MosaicRows)
-        L.mosaic_qk_norm_rope.argtypes = [rows, rows, rows] + [C.c_int32] * 6 + [vp, vp, C.c_float, vp, C.c_int32, st3, vp, C.c_int32,
-                                                                               C.c_int32, vp]
-        L.mosaic_quant_append.argtypes = [qc, vp, vp, st3, st3, vp, C.c_int32, vp]
+        qc = C.POINTER(MosaicQuantCache)                   # (rows and strides also come as packed bytes)
+        L.mosaic_qk_norm_rope.argtypes = [vp, vp, vp] + [C.c_int32] * 6 + [vp, vp, C.c_float, vp, C.c_int32, vp, vp, C.c_int32, C.c_int32,
+                                                                         vp]
+        L.mosaic_quant_append.argtypes = [qc, vp, vp, vp, vp, vp, C.c_int32, vp]
         L.mosaic_quant_workspace_bytes.argtypes = [qc, C.POINTER(sz)]
         L.mosaic_quant_decode_attention.argtypes = [qc, vp, vp, C.c_float, vp, sz, vp]
         L.mosaic_quant_select_attention.argtypes = [qc, vp, vp, C.c_float, C.c_int32, C.c_int32, vp, vp, sz, vp]
