@@ -460,8 +460,9 @@ mosaic_status mosaic_dense_decode_attention(const void *q, const void *k, const 
  *                  up to 2^53
  *   inv_freq     : fp32 [rot_dim / 2]; rot_dim is a multiple of 16 up to 128
  * Strides are host arrays.  num_seqs or num_tokens 0: OK, nothing enqueued.
+ * A row with a NaN or an infinity spoils itself only.
  * Errors: INVALID (NULL, shape, alignment, strides), UNSUPPORTED (head_dim
- * != 128, rot_dim, more than 2^31 - 1 tokens). */
+ * != 128, rot_dim, 2^23 tokens or more). */
 typedef struct {
     const void *in;
     void *out;
@@ -513,8 +514,8 @@ typedef struct {
  *          rows from new_lens[s] on are not read
  * The lengths are known on the device only: a sequence that has no room for all
  * of its new tokens takes none of them, and its entry of `refused` counts up.
- * Errors: INVALID, UNSUPPORTED (head_dim, block_len), CAPACITY (max_new exceeds
- * a sequence's room with new_lens NULL). */
+ * Errors: INVALID, UNSUPPORTED (head_dim, block_len, max_new of 2^28 or more),
+ * CAPACITY (max_new exceeds a sequence's room with new_lens NULL). */
 mosaic_status mosaic_quant_append(const mosaic_quant_cache *cache, const void *k, const void *v,
                                   const int64_t *k_strides_host, const int64_t *v_strides_host, const int32_t *new_lens,
                                   int32_t max_new, void *stream);
@@ -530,7 +531,7 @@ mosaic_status mosaic_quant_workspace_bytes(const mosaic_quant_cache *cache, size
  *   q   : [S][H * group_size][128] (cache dtype), 16-byte aligned
  *   out : [S][H * group_size][128] fp32
  *   ws  : at least mosaic_quant_workspace_bytes bytes, 256-byte aligned
- * A sequence without tokens gets zeros. */
+ * A sequence without tokens gets zeros.  Logits must stay within fp32. */
 mosaic_status mosaic_quant_decode_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,
                                             void *ws, size_t ws_bytes, void *stream);
 

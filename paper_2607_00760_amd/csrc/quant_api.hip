@@ -27,6 +27,8 @@ mosaic_status done(hipError_t e, const char *what) {
     return MOSAIC_OK;
 }
 
+constexpr int MAX_THREADS = 0x7fffffff;                    // of a launch along its first dimension
+
 bool off16(const void *p) { return (uintptr_t)p % 16 != 0; }
 uint64_t align256(uint64_t x) { return (x + 255) & ~uint64_t(255); }
 
@@ -108,7 +110,7 @@ mosaic_status mosaic_quant_append(const mosaic_quant_cache *c, const void *k, co
     const long long room = (long long)c->max_blocks * c->block_len;
     if (!new_lens && max_new > room) return fail(MOSAIC_ERR_CAPACITY, "%d tokens for a cache of %lld", max_new, room);
     if (max_new == 0) return done(hipSuccess, "");
-    if (max_new > 0x3fffffff) return fail(MOSAIC_ERR_UNSUPPORTED, "max_new %d", max_new);
+    if (max_new > MAX_THREADS / 8) return fail(MOSAIC_ERR_UNSUPPORTED, "max_new %d: at most %d", max_new, MAX_THREADS / 8);
     const QNew n{(const uint16_t *)k, (const uint16_t *)v, k_strides[0], k_strides[1], k_strides[2], v_strides[0], v_strides[1],
                  v_strides[2], new_lens, max_new};
     return done(launch_quant_append(q, c->format, c->block_len, c->dtype, n, (hipStream_t)stream), "append launch");
@@ -160,7 +162,8 @@ mosaic_status mosaic_qk_norm_rope(const mosaic_rows *q, const mosaic_rows *k, co
     if (pos_bytes != 4 && pos_bytes != 8) return fail(MOSAIC_ERR_INVALID, "pos_bytes %d", pos_bytes);
     if (!q_weight != !k_weight) return fail(MOSAIC_ERR_INVALID, "weights of both queries and keys, or of neither");
     if (!(eps >= 0.0f)) return fail(MOSAIC_ERR_INVALID, "eps %g", (double)eps);
-    if ((long long)num_seqs * num_tokens > 0x7fffffff) return fail(MOSAIC_ERR_UNSUPPORTED, "%d x %d tokens", num_seqs, num_tokens);
+    if ((long long)num_seqs * num_tokens > MAX_THREADS / 256)
+        return fail(MOSAIC_ERR_UNSUPPORTED, "%d x %d tokens: at most %d", num_seqs, num_tokens, MAX_THREADS / 256);
     if ((uintptr_t)positions % pos_bytes || (uintptr_t)inv_freq % 4 || off16(q_weight) || off16(k_weight))
         return fail(MOSAIC_ERR_INVALID, "misaligned positions, inv_freq or weights");
     const mosaic_rows *rows[3] = {q, k, v};

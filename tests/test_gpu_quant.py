@@ -25,7 +25,7 @@ def tokens(g, *shape, dt, strong=8.0):
 
 
 def make(fmt, dtype, block, S, H, G, cap, fill=None):
-    """A cache whose unwritten parts hold `fill` in every byte (0x7f: NaN codes, NaN or large 16-bit values)."""
+    """A cache whose unwritten parts hold `fill` in every byte (0xff: NaN scales, codes and 16-bit values)."""
     c = M.QuantCache(M.QuantParams(H, G, dtype, fmt, block), S, cap)
     if fill is not None:
         for n in c.TENSORS:
@@ -80,7 +80,7 @@ def test_append_in_any_pieces(fmt, dtype, block):
     total = [sum(x[s] for x in steps) for s in range(S)]
     assert max(total) <= cap
     k, v = tokens(g, S, H, max(total), dt=dt), tokens(g, S, H, max(total), dt=dt, strong=1.0)
-    c = make(fmt, dtype, block, S, H, 4, cap, 0x7f)
+    c = make(fmt, dtype, block, S, H, 4, cap, 0xff)
     at = [0] * S
     for i, counts in enumerate(steps):
         m = max(counts)
@@ -96,7 +96,7 @@ def test_append_in_any_pieces(fmt, dtype, block):
             kc, vc = kc[:, :, 0], vc[:, :, 0]
         c.append(kc, vc, torch.tensor(counts, dtype=torch.int32, device="cuda"))
     pairs = {(s, h): R.Pair(k[s, h, : total[s]], v[s, h, : total[s]], fmt, block) for s in range(S) for h in range(H)}
-    same_state(c, pairs, 0x7f)
+    same_state(c, pairs, 0xff)
     assert not c.refused.any()
 
 
@@ -125,7 +125,7 @@ def test_append_without_room():
     B, S, H, dt = 32, 3, 2, torch.float16
     g = torch.Generator().manual_seed(1)
     k, v = tokens(g, S, H, 2 * B, dt=dt), tokens(g, S, H, 2 * B, dt=dt)
-    c = make("e4m3", "fp16", B, S, H, 1, 2 * B - 5, 0x7f)
+    c = make("e4m3", "fp16", B, S, H, 1, 2 * B - 5, 0xff)
     assert c.max_tokens == 2 * B
     n = torch.tensor([2 * B, B, 0], dtype=torch.int32, device="cuda")
     c.append(k.cuda(), v.cuda(), n)
@@ -137,7 +137,7 @@ def test_append_without_room():
         pairs[0, h] = R.Pair(k[0, h], v[0, h], "e4m3", B)
         pairs[1, h] = R.Pair(torch.cat((k[1, h, :B], k[1, h, :1])), torch.cat((v[1, h, :B], v[1, h, :1])), "e4m3", B)
         pairs[2, h] = R.Pair(k[2, h, :1], v[2, h, :1], "e4m3", B)
-    same_state(c, pairs, 0x7f)
+    same_state(c, pairs, 0xff)
     with pytest.raises(M.MosaicError):
         c.append(torch.zeros(S, H, 2 * B + 1, D, dtype=dt, device="cuda"), torch.zeros(S, H, 2 * B + 1, D, dtype=dt, device="cuda"))
     c.reset([1])
@@ -160,7 +160,7 @@ def test_decode_and_selection_at_the_edges(fmt, dtype, block, G):
     g = torch.Generator().manual_seed(G)
     k, v = tokens(g, S, H, max(lens), dt=dt), tokens(g, S, H, max(lens), dt=dt, strong=1.0)
     q = tokens(g, S, H * G, dt=dt, strong=1.0)
-    c = make(fmt, dtype, block, S, H, G, max(lens), 0x7f)
+    c = make(fmt, dtype, block, S, H, G, max(lens), 0xff)
     c.append(k.cuda(), v.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
     out = c.decode(q.cuda(), SCALE)
     blocks = torch.empty_like(c.k_scale, dtype=torch.int32)
@@ -198,7 +198,7 @@ def test_decode_scales_that_differ(fmt, dtype, block):
     q[0, 2] = 0.0
     q[0, 3] *= 30.0
     q = q.to(dt)
-    c = make(fmt, dtype, block, 1, 1, G, n, 0x7f)
+    c = make(fmt, dtype, block, 1, 1, G, n, 0xff)
     c.append(k.cuda(), v.cuda())
     out = c.decode(q.cuda(), SCALE)
     r = R.Pair(k[0, 0], v[0, 0], fmt, block)
@@ -242,7 +242,7 @@ def test_uneven_batches_share_the_work(S, H):
     g = torch.Generator(device="cuda").manual_seed(S)
     k, v = (torch.randn(S, H, max(lens), D, generator=g, device="cuda").to(dt) for _ in range(2))
     q = torch.randn(S, H * G, D, generator=g, device="cuda").to(dt)
-    c = make("int8", "fp16", B, S, H, G, max(lens), 0x7f)
+    c = make("int8", "fp16", B, S, H, G, max(lens), 0xff)
     c.append(k, v, torch.tensor(lens, dtype=torch.int32, device="cuda"))
     out, part = c.decode(q, SCALE), c.decode_selected(q, SCALE, (1, 5))
     for s in [s for s in range(S) if lens[s] > 1000 or s % 13 == 0 or s % 9 == 4]:
@@ -306,7 +306,7 @@ def test_steps_together_captured_and_eager(select):
     k, v = tokens(g, S, H, 300, dt=dt).cuda(), tokens(g, S, H, 300, dt=dt).cuda()
     new = tokens(g, steps, S, (G + 2) * H, dt=dt, strong=1.0).flatten(2).cuda()
     n = torch.tensor(prompt, dtype=torch.int32, device="cuda")
-    caches = [make("e4m3", "bf16", B, S, H, G, 300 + steps, 0x7f) for _ in range(3)]
+    caches = [make("e4m3", "bf16", B, S, H, G, 300 + steps, 0xff) for _ in range(3)]
     for c in caches:
         c.append(k, v, n)
     want = [_step(caches[0], new[t], inv, w, H, G, select) for t in range(steps)]

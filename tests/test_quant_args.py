@@ -79,6 +79,7 @@ def test_arguments_that_are_refused(lib):
                dict(vs=three(8196, 1024, 128)), dict(n=-1), dict(lens=FAKE + 1)):
         refused(lib, INVALID, lambda: append(lib, c, **kw))
     refused(lib, CAPACITY, lambda: append(lib, c, n=3201))
+    refused(lib, UNSUPPORTED, lambda: append(lib, c, n=1 << 28, lens=FAKE))
     for call in (decode, select):
         for kw in (dict(q=None), dict(out=None), dict(ws=None), dict(q=FAKE + 8), dict(out=FAKE + 2), dict(ws=FAKE + 16),
                    dict(nbytes=n.value - 1)):
@@ -113,7 +114,7 @@ def test_norm_rope_refusals(lib):
                dict(hkv=0), dict(pb=2), dict(qw=None), dict(kw=None), dict(eps=-1.0), dict(eps=float("nan")), dict(pos=FAKE + 2),
                dict(pos=FAKE + 4, pb=8), dict(inv=FAKE + 2), dict(qw=FAKE + 8), dict(kw=FAKE + 2)):
         refused(lib, INVALID, lambda: rope(lib, **kw))
-    for kw in (dict(d=64), dict(rot=0), dict(rot=20), dict(rot=144), dict(S=1 << 20, n=1 << 12)):
+    for kw in (dict(d=64), dict(rot=0), dict(rot=20), dict(rot=144), dict(S=1 << 20, n=1 << 12), dict(n=1 << 22)):
         refused(lib, UNSUPPORTED, lambda: rope(lib, **kw))
     lib.fake_reset(-1)
     assert rope(lib, S=0) == OK and rope(lib, n=0) == OK and lib.fake_calls() == 0
