@@ -44,9 +44,10 @@ struct QPlan {
     bool live;
 };
 
-// units(L): units of a pair of L tokens; least: runs of a pair at least.
+// units(L): units of a pair of L tokens; least: runs of a pair at least; alone:
+// units that a pair's only run may have, whatever c is.
 template <typename U>
-__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int step, int least, U units, int w) {
+__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int step, int least, int alone, U units, int w) {
     const int lane = threadIdx.x & 63;
     auto length = [&](int s) { return s < q.S ? q.len((long long)s * q.H) : 0; };
     const int L0 = length(lane);
@@ -60,13 +61,15 @@ __device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, in
     uint32_t base = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
         const int s = s0 + lane, L = s0 ? length(s) : L0;
-        const int ns = s < q.S ? max(least, (units(L) + c - 1) / c) : 0;
+        const int u = s < q.S ? units(L) : 0;
+        const int ns = s < q.S ? max(least, u <= alone ? min(u, 1) : (u + c - 1) / c) : 0;
         const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
         const uint64_t hit = __ballot(base + inc > (uint32_t)w);       // the first sequence whose runs end past w
         if (hit) {
             const int l = (int)__builtin_ctzll(hit);
             p.s = s0 + l;
             p.ns = __builtin_amdgcn_readlane(ns, l);
+            if (p.ns == 1) p.c = max(c, alone);
             p.L = __builtin_amdgcn_readlane(L, l);
             const int r = w - ((int)(base + (uint32_t)__builtin_amdgcn_readlane((int)inc, l)) - p.ns * q.H);
             p.h = r / p.ns;

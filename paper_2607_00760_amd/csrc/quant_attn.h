@@ -32,6 +32,7 @@ __host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256
 // Blocks of a run at least: two steps a wave.  1 x 4117 tokens, 8 kv heads: 4
 // blocks 11.5 us, 8 9.6, 16 11.7 (a step costs less than joining twice the runs).
 constexpr int QA_LEAST = 2 * QA_NWV;
+constexpr int QA_ALONE = 16;                               // units of a pair that one run takes: joining costs 3 us
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and accumulators of the heads
 
@@ -141,7 +142,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     __shared__ int last;
     auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
     auto units = [&](int L) { return blocks(L) + (L % B != 0); };        // the unfinished block is a pair's last unit
-    const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_LEAST, QA_NWV, 1, units, blockIdx.x);
+    const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_LEAST, QA_NWV, 1, QA_ALONE, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -18,9 +18,8 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
-constexpr int QS_UNIT = 64;                                // blocks of a workgroup's step, 16 a wave
-constexpr int QS_RUNS = 1024;                              // runs of a launch, about
-constexpr int QS_AHEAD = 4;
+constexpr int QS_UNIT = 64;                                // blocks of a scoring workgroup's step, 16 a wave
+constexpr int QS_RUNS = 1024;                              // runs of a scoring launch, about
 
 // codes of 16 channels of a query in 8-bit integers, one half of them zeroed
 __device__ __forceinline__ i32x4 pack_signed(const float (&x)[16], bool upper) {
@@ -38,52 +37,40 @@ __device__ __forceinline__ i32x4 pack_signed(const float (&x)[16], bool upper) {
     return r;
 }
 
-// grid QS_RUNS + pairs: one run of 64-block units of a pair each.  A wave has
-// QS_AHEAD steps of 16 blocks in flight; the first are out before the query is
-// looked at.
-template <int DT>
-__global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores, int32_t *list) {
-    const QPlan pl = q_plan(q, QS_RUNS, 1, 1, 0, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
-    if (!pl.live) return;
-    const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int p = pl.s * q.H + pl.h, nb = pl.L / block;
+// The scores of blocks [b, b1) of pair p (nb blocks), a wave's 16 from b and
+// then every `step`: emit(block, score).  QS_AHEAD steps are in flight, the
+// first before the query is looked at.  (Loads past the end read the last
+// block again: a branch around each would wait for those before it.)
+template <int DT, int QS_AHEAD, typename E>
+__device__ __forceinline__ void score_blocks(const QCache &q, int p, int nb, const uint16_t *query, int b, int b1, int step, E emit) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
     const int8_t *bp = q.bounds + (uint64_t)p * q.N * (2 * D);
     const float *bs = q.bs + (uint64_t)p * q.N;
-    float *out = scores + (uint64_t)p * q_score_stride(q.N);
-    int b = pl.i * pl.c * QS_UNIT + 16 * wave;
-    const int b1 = min(nb, (pl.i + 1) * pl.c * QS_UNIT);
+    if (b >= b1) return;
     i32x4 w[QS_AHEAD][4];
-    float u[QS_AHEAD][4];
-    auto load = [&] {
+    float u[QS_AHEAD];                                     // of block 4 q4 + l16 % 4
+    auto load = [&](int s, int at) {
+        const i32x4 *row = (const i32x4 *)(bp + (uint64_t)min(at + l16, nb - 1) * (2 * D)) + q4;
 #pragma unroll
-        for (int a = 0; a < QS_AHEAD; ++a) {
-            const int at = b + a * QS_UNIT;
-            if (at < b1) {
-                const i32x4 *row = (const i32x4 *)(bp + (uint64_t)min(at + l16, nb - 1) * (2 * D)) + q4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[a][e] = row[4 * e];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) u[a][r] = bs[min(at + 4 * q4 + r, nb - 1)];
-            }
-        }
+        for (int e = 0; e < 4; ++e) w[s][e] = row[4 * e];
+        u[s] = bs[min(at + 4 * q4 + (l16 & 3), nb - 1)];
     };
-    load();
-    {                                                      // the list's places, -1 until the selection takes them
-        int32_t *lp = list + (uint64_t)p * q.N;
-        const int e1 = pl.i == pl.ns - 1 ? q.N : b1;
-        for (int e = pl.i * pl.c * QS_UNIT + threadIdx.x; e < e1; e += 256) lp[e] = -1;
-    }
+#pragma unroll
+    for (int s = 0; s < QS_AHEAD; ++s) load(s, b + s * step);
     const int head = min(l16, q.G - 1);                    // columns past the group repeat its last head
     const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
     float x[2][16];
     float a = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
+    for (int e = 0; e < 2; ++e) {
+        uint16_t h[16];
+        __builtin_memcpy(h, __builtin_assume_aligned(qp + 64 * e + 16 * q4, 16), 32);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            x[e][i] = h2f(qp[64 * e + 16 * q4 + i], DT);
+            x[e][i] = h2f(h[i], DT);
             a = fmaxf(a, fabsf(x[e][i]));
         }
+    }
     a = fmaxf(rows_all(a, [](float m, float o) { return fmaxf(m, o); }), QLEAST);
     const float inv = 127.0f / a, unit = a / 127.0f;
 #pragma unroll
@@ -91,46 +78,69 @@ __global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const 
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[e][i] = rintf(x[e][i] * inv);
     const i32x4 qb[4] = {pack_signed(x[0], true), pack_signed(x[1], true), pack_signed(x[0], false), pack_signed(x[1], false)};
-    while (b < b1) {
+    auto score = [&](int s, int at) {
+        i32x4 acc = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s][e], qb[e], acc, 0, 0, 0);
+        float sc[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {                      // block at + 4 q4 + r: the largest over the heads
+            sc[r] = (float)acc[r] * unit;
+            sc[r] = fmaxf(sc[r], dpp_read<0x128, 0xf>(sc[r]));
+            sc[r] = fmaxf(sc[r], dpp_read<0x124, 0xf>(sc[r]));
+            sc[r] = fmaxf(sc[r], dpp_read<0x122, 0xf>(sc[r]));
+            sc[r] = fmaxf(sc[r], dpp_read<0x121, 0xf>(sc[r]));
+        }
+        const float mine = (l16 & 2) ? ((l16 & 1) ? sc[3] : sc[2]) : ((l16 & 1) ? sc[1] : sc[0]);
+        const int blk = at + 4 * q4 + l16;
+        if (l16 < 4 && blk < b1) emit(blk, mine * u[s]);
+    };
+    for (; b + QS_AHEAD * step < b1; b += QS_AHEAD * step)
 #pragma unroll
         for (int s = 0; s < QS_AHEAD; ++s) {
-            if (b + s * QS_UNIT >= b1) break;
-            i32x4 acc = i32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s][e], qb[e], acc, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {                  // block at + 4 q4 + r, head l16
-                float sc = (float)acc[r] * unit;
-                sc = fmaxf(sc, dpp_read<0x128, 0xf>(sc));
-                sc = fmaxf(sc, dpp_read<0x124, 0xf>(sc));
-                sc = fmaxf(sc, dpp_read<0x122, 0xf>(sc));
-                sc = fmaxf(sc, dpp_read<0x121, 0xf>(sc));
-                const int at = b + s * QS_UNIT + 4 * q4 + r;
-                if (l16 == r && at < b1) out[at] = sc * u[s][r];
-            }
+            score(s, b + s * step);
+            load(s, b + (s + QS_AHEAD) * step);
         }
-        b += QS_AHEAD * QS_UNIT;
-        if (b < b1) load();
-    }
+#pragma unroll
+    for (int s = 0; s < QS_AHEAD; ++s) score(s, b + s * step);
 }
 
-// The `want` best scores of a pair, one workgroup of 16 waves: thread t owns
-// the KPT consecutive blocks from KPT t (KPT = 0: as many as it takes, read
-// again from memory in each pass).  A radix selection over the range of the
-// keys: a pass of 2048 bins narrows the candidates to the threshold's bin;
-// where that holds up to 64 of them (mostly after the first) every wave ranks
-// them itself, a lane each.  Blocks above the threshold are taken, those equal
-// to it in block order while they are needed; one scan places them in
-// ascending order.
-template <int KPT>
-__global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int num, int den, const float *scores, int32_t *list) {
-    constexpr int NW = 16, NT = 64 * NW, BINS = 2048, BPT = BINS / NT, FEW = 64;
-    __shared__ uint32_t hist[2][BINS];
-    __shared__ uint32_t mm[2 * NW], pk[NW], pub[3], sc[2][NW], few[FEW], cmp[FEW], nfew;
-    const int p = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const int nb = q.len(p) / block, want = q_want(nb, num, den);
-    const float *src = scores + (uint64_t)p * q_score_stride(q.N);
-    int32_t *dst = list + (uint64_t)p * q.N;
+// grid QS_RUNS + pairs: one run of 64-block units of a pair each
+template <int DT>
+__global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores, int32_t *list) {
+    const QPlan pl = q_plan(q, QS_RUNS, 1, 1, 0, 0, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
+    if (!pl.live) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int p = pl.s * q.H + pl.h, nb = pl.L / block;
+    const int b0 = pl.i * pl.c * QS_UNIT, b1 = min(nb, b0 + pl.c * QS_UNIT);
+    {                                                      // the list's places, -1 until the selection takes them
+        int32_t *lp = list + (uint64_t)p * q.N;
+        const int e1 = pl.i == pl.ns - 1 ? q.N : b1;
+        for (int e = b0 + threadIdx.x; e < e1; e += 256) lp[e] = -1;
+    }
+    float *out = scores + (uint64_t)p * q_score_stride(q.N);
+    auto emit = [&](int at, float s) { out[at] = s; };
+    if (pl.c == 1) score_blocks<DT, 1>(q, p, nb, query, b0 + 16 * wave, b1, QS_UNIT, emit);
+    else score_blocks<DT, 4>(q, p, nb, query, b0 + 16 * wave, b1, QS_UNIT, emit);
+}
+
+// The `want` (at least one) best of a pair's scores src[0, nb), by one workgroup
+// of NW waves: thread t owns the KPT consecutive blocks from KPT t (KPT = 0: as
+// many as it takes, read again in each pass).  A radix selection over the range
+// of the keys: a pass of 2048 bins narrows the candidates to the threshold's
+// bin; where that holds up to 64 of them (mostly after the first) the waves
+// rank them, a lane each.  Blocks above the threshold are taken, those equal to
+// it in block order while they are needed; one scan places them in ascending
+// order.
+constexpr int QK_BINS = 2048, QK_FEW = 64;
+template <int QK_NW> struct PickSmem {
+    uint32_t hist[2][QK_BINS];
+    uint32_t mm[2 * QK_NW], pk[QK_NW], pub[3], sc[2][QK_NW], few[QK_FEW], cmp[QK_FEW], nfew;
+};
+template <int KPT, int NW>
+__device__ __forceinline__ void pick(const float *src, int nb, int want, int32_t *dst, PickSmem<NW> &sm) {
+    constexpr int NT = 64 * NW, BINS = QK_BINS, BPT = BINS / NT, FEW = QK_FEW;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int own = KPT ? KPT : (nb + NT - 1) / NT;
     const int i0 = min(nb, tid * own), n_own = min(nb, i0 + own) - i0;
     uint32_t kr[KPT ? KPT : 1];
@@ -146,13 +156,9 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
             kr[4 * e + 3] = score_key(f[e].w);
         }
     }
-    for (int i = tid; i < BINS; i += NT) hist[0][i] = 0u;
-    if (tid == 0) nfew = 0u;
-    if (tid < FEW) cmp[tid] = 0u;
-    if (want == 0) {                                       // (no scores were made)
-        for (int i = tid; i < q.N; i += NT) dst[i] = -1;
-        return;
-    }
+    for (int i = tid; i < BINS; i += NT) sm.hist[0][i] = 0u;
+    if (tid == 0) sm.nfew = 0u;
+    if (tid < FEW) sm.cmp[tid] = 0u;
     auto each = [&](auto f) {
         if (KPT) {
 #pragma unroll
@@ -166,13 +172,13 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
     each([&](int, uint32_t k) { kmin = min(kmin, k); kmax = max(kmax, k); });
     kmin = ~wave_max_u(~kmin);
     kmax = wave_max_u(kmax);
-    if (lane == 0) { mm[wv] = kmin; mm[NW + wv] = kmax; }
+    if (lane == 0) { sm.mm[wv] = kmin; sm.mm[NW + wv] = kmax; }
     lds_barrier();
-    kmin = ~wave_max_u(lane < NW ? ~mm[lane] : 0u);
-    kmax = wave_max_u(lane < NW ? mm[NW + lane] : 0u);
+    kmin = ~wave_max_u(lane < NW ? ~sm.mm[lane] : 0u);
+    kmax = wave_max_u(lane < NW ? sm.mm[NW + lane] : 0u);
     uint32_t base = kmin, span = kmax - kmin, rem = (uint32_t)want;    // candidates: [base, base + span]
     for (int pass = 0;; ++pass) {
-        uint32_t *hc = hist[pass & 1], *hn = hist[(pass + 1) & 1];
+        uint32_t *hc = sm.hist[pass & 1], *hn = sm.hist[(pass + 1) & 1];
         const int bits = 32 - (span ? __builtin_clz(span) : 32), sh = bits > 11 ? bits - 11 : 0;
         each([&](int, uint32_t k) { if (k >= base && k - base <= span) atomicAdd(&hc[(k - base) >> sh], 1u); });
         lds_barrier();
@@ -181,33 +187,33 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
 #pragma unroll
         for (int e = 0; e < BPT; ++e) { hb[e] = hc[b0 + e]; mine += hb[e]; hn[b0 + e] = 0u; }
         uint32_t tot;
-        uint32_t above = block_excl<NW>(mine, tot, pk);
+        uint32_t above = block_excl<NW>(mine, tot, sm.pk);
         if (above < rem && above + mine >= rem) {
 #pragma unroll
             for (int e = BPT - 1; e >= 0; --e) {
-                if (above < rem && above + hb[e] >= rem) { pub[0] = (uint32_t)(b0 + e); pub[1] = rem - above; pub[2] = hb[e]; }
+                if (above < rem && above + hb[e] >= rem) { sm.pub[0] = (uint32_t)(b0 + e); sm.pub[1] = rem - above; sm.pub[2] = hb[e]; }
                 above += hb[e];
             }
         }
         lds_barrier();
-        base += pub[0] << sh;
-        span = min(span - (pub[0] << sh), sh ? (1u << sh) - 1u : 0u);
-        rem = pub[1];
+        base += sm.pub[0] << sh;
+        span = min(span - (sm.pub[0] << sh), sh ? (1u << sh) - 1u : 0u);
+        rem = sm.pub[1];
         if (sh == 0) break;                                // single keys: the threshold is base
-        if (pub[2] <= FEW) {                               // (once: the loop ends here)
-            const int n = (int)pub[2];
-            each([&](int, uint32_t k) { if (k >= base && k - base <= span) few[atomicAdd(&nfew, 1u)] = k; });
+        if (sm.pub[2] <= FEW) {                            // (once: the loop ends here)
+            const int n = (int)sm.pub[2];
+            each([&](int, uint32_t k) { if (k >= base && k - base <= span) sm.few[atomicAdd(&sm.nfew, 1u)] = k; });
             lds_barrier();
             // a wave compares every candidate, a lane each, with its share of them
-            const uint32_t k = lane < n ? few[lane] : 0u;
+            const uint32_t k = lane < n ? sm.few[lane] : 0u;
             uint32_t c = 0u;                               // candidates above, and from bit 16 equal ones
             for (int e = wv; e < n; e += NW) {
                 const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)k, e);
                 c += o > k ? 1u : (o == k ? 0x10000u : 0u);
             }
-            if (c) atomicAdd(&cmp[lane], c);
+            if (c) atomicAdd(&sm.cmp[lane], c);
             lds_barrier();
-            const uint32_t gt = cmp[lane] & 0xffffu, ge = gt + (cmp[lane] >> 16);
+            const uint32_t gt = sm.cmp[lane] & 0xffffu, ge = gt + (sm.cmp[lane] >> 16);
             const int l = (int)__builtin_ctzll(__ballot(lane < n && gt < rem && ge >= rem));   // (rem of the n are needed: never empty)
             base = (uint32_t)__builtin_amdgcn_readlane((int)k, l);
             rem -= (uint32_t)__builtin_amdgcn_readlane((int)gt, l);
@@ -217,8 +223,8 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
     // taken: above the threshold, or equal to it while the equal ones before are fewer than rem
     uint32_t eq = 0u, gt = 0u, tot;
     each([&](int, uint32_t k) { eq += k == base ? 1u : 0u; gt += k > base ? 1u : 0u; });
-    uint32_t before = block_excl<NW>(eq, tot, sc[0]);
-    uint32_t pos = block_excl<NW>(gt + min(eq, rem > before ? rem - before : 0u), tot, sc[1]);
+    uint32_t before = block_excl<NW>(eq, tot, sm.sc[0]);
+    uint32_t pos = block_excl<NW>(gt + min(eq, rem > before ? rem - before : 0u), tot, sm.sc[1]);
     each([&](int e, uint32_t k) {
         const bool t = k > base || (k == base && before < rem);
         before += k == base ? 1u : 0u;
@@ -226,11 +232,51 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
     });
 }
 
+template <int KPT>
+__global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int num, int den, const float *scores, int32_t *list) {
+    __shared__ PickSmem<16> sm;
+    const int p = blockIdx.x, nb = q.len(p) / block, want = q_want(nb, num, den);
+    int32_t *dst = list + (uint64_t)p * q.N;
+    if (want == 0) {                                       // (no scores were made)
+        for (int i = threadIdx.x; i < q.N; i += 1024) dst[i] = -1;
+        return;
+    }
+    pick<KPT, 16>(scores + (uint64_t)p * q_score_stride(q.N), nb, want, dst, sm);
+}
+
+// Scores and selection of a pair of up to QK_FUSED blocks in one workgroup, the
+// scores in LDS.  It saves a launch (2 us), and a compute unit reads 32 bytes a
+// ns at most, whoever asks: so for caches of up to 256 blocks a pair, and for
+// larger ones where there are pairs for half of the chip.  Whole calls, blocks
+// of 32, 8 kv heads, us in one workgroup / spread over several:
+//   tokens       2048         8192         16384        32768
+//   1 sequence   13.3 / 14.7  16.2 / 17.4  17.9 / 17.4  22.2 / 18.1
+//   16           13.3 / 14.9  20.6 / 22.6  26.7 / 28.7  45.2 / 48.7
+constexpr int QK_FUSED = 1024, QK_NW = 4;
+template <int DT>
+__global__ void __launch_bounds__(64 * QK_NW) k_quant_pick(QCache q, int block, const uint16_t *query, int num, int den, int32_t *list) {
+    __shared__ PickSmem<QK_NW> sm;
+    __shared__ __align__(16) float scores[QK_FUSED];
+    const int p = blockIdx.x, nb = q.len(p) / block, want = q_want(nb, num, den);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t *dst = list + (uint64_t)p * q.N;
+    for (int i = want + threadIdx.x; i < q.N; i += 64 * QK_NW) dst[i] = -1;
+    if (want == 0) return;
+    score_blocks<DT, 4>(q, p, nb, query, 16 * wave, nb, 16 * QK_NW, [&](int at, float s) { scores[at] = s; });
+    lds_barrier();
+    pick<4, QK_NW>(scores, nb, want, dst, sm);
+}
+
 }  // namespace
 
 hipError_t launch_quant_select(const QCache &q, int block, int dtype, const uint16_t *query, int num, int den, float *scores,
                                int32_t *list, hipStream_t s) {
     const int pairs = q.S * q.H;
+    if (q.N <= 256 || (q.N <= QK_FUSED && pairs >= 128)) {
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(pairs), dim3(64 * QK_NW), 0, s, q, block, query, num, den, list); };
+        if (dtype) go(k_quant_pick<1>); else go(k_quant_pick<0>);
+        return hipGetLastError();
+    }
     const long long most = (long long)pairs * ceil_div(q.N, QS_UNIT);
     const dim3 grid((uint32_t)(most < QS_RUNS + pairs ? most : QS_RUNS + pairs));
     if (dtype) hipLaunchKernelGGL(k_quant_score<1>, grid, dim3(256), 0, s, q, block, query, scores, list);
