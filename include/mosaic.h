@@ -521,7 +521,7 @@ mosaic_status mosaic_quant_append(const mosaic_quant_cache *cache, const void *k
                                   int32_t max_new, void *stream);
 
 /* Workspace of the two attentions below (depends on the cache's shape only).
- * Its first 256 KiB must be zero before its first use; every call leaves them
+ * Its first 512 KiB must be zero before its first use; every call leaves them
  * so, and caches of other shapes may use it in turn if it is large enough.
  * Calls that overlap on one workspace race; separate streams need their own. */
 mosaic_status mosaic_quant_workspace_bytes(const mosaic_quant_cache *cache, size_t *bytes);

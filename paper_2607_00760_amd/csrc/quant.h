@@ -95,8 +95,10 @@ struct QSel {                                              // a selection, or li
 
 // ---------------------------------------------------------------- launchers
 hipError_t launch_quant_append(const QCache &q, int fmt, int block, int dtype, const QNew &n, hipStream_t s);
-constexpr int Q_PAIRS = 65535;                             // pairs at most
-// the attention's workspace: arrivals [Q_PAIRS + 1] (zero between calls), then partials
+constexpr int Q_PAIRS = 64512;                             // pairs at most, and runs
+constexpr int Q_RUNS = 65536;
+// the attention's workspace: arrivals at pairs and at groups of runs [2][Q_RUNS]
+// (zero between calls), then partials
 size_t quant_attn_ws_bytes(int pairs);
 hipError_t launch_quant_attn_e4m3(const QCache &q, int block, int dtype, const uint16_t *query, float scale, const QSel &sel,
                                   void *ws, float *out, hipStream_t s);

@@ -72,10 +72,11 @@ __device__ __forceinline__ float2 get2(const float *p) {
     return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
-// The partials of ns runs to a pair's outputs: a thread takes four columns of
-// every np-th run, np = 256 / (32 G) shares, joined in LDS.  The loads of 8
-// runs are out together.
-__device__ __forceinline__ void join_runs(const float *part, int ns, int G, float *lds, float *out) {
+// ns partials, `stride` floats apart, joined: a thread takes four columns of
+// every np-th one, np = 256 / (32 G) shares, joined in LDS; the loads of 8 are
+// out together.  The result is that of threads [0, 32 G).
+struct Joined { float M, S; float4 A; };
+__device__ __forceinline__ Joined join_runs(const float *part, int stride, int ns, int G, float *lds) {
     constexpr int CB = 8;
     const int tid = threadIdx.x, cols = 32 * G, np = 64 * QA_NWV / cols;
     const int share = tid / cols, col = tid - share * cols, h = col >> 5;
@@ -86,7 +87,7 @@ __device__ __forceinline__ void join_runs(const float *part, int ns, int G, floa
             float2 ml[CB], a[CB][2];
 #pragma unroll
             for (int e = 0; e < CB; ++e) {
-                const float *ps = part + (uint64_t)min(r0 + e * np, ns - 1) * QA_PART;
+                const float *ps = part + (uint64_t)min(r0 + e * np, ns - 1) * stride;
                 ml[e] = get2(ps + 2 * h);
                 a[e][0] = get2(ps + 2 * QA_HEADS + 4 * col);
                 a[e][1] = get2(ps + 2 * QA_HEADS + 4 * col + 2);
@@ -119,18 +120,39 @@ __device__ __forceinline__ void join_runs(const float *part, int ns, int G, floa
         x[5] = S;
     }
     __syncthreads();
-    if (share > 0) return;
-    for (int e = 1; e < np; ++e) {
-        const float *o = lds + 8 * (tid + e * cols);
-        const float4 a = *(const float4 *)o;
-        const float mn = fmaxf(M, o[4]), mb = mn == -INFINITY ? 0.0f : mn;
-        const float x = __builtin_amdgcn_exp2f(M - mb), y = __builtin_amdgcn_exp2f(o[4] - mb);
-        A = make_float4(A.x * x + a.x * y, A.y * x + a.y * y, A.z * x + a.z * y, A.w * x + a.w * y);
-        S = S * x + o[5] * y;
-        M = mn;
-    }
-    *(float4 *)(out + 4 * col) = make_float4(joined(A.x, S), joined(A.y, S), joined(A.z, S), joined(A.w, S));
+    if (share == 0)
+        for (int e = 1; e < np; ++e) {
+            const float *o = lds + 8 * (tid + e * cols);
+            const float4 a = *(const float4 *)o;
+            const float mn = fmaxf(M, o[4]), mb = mn == -INFINITY ? 0.0f : mn;
+            const float x = __builtin_amdgcn_exp2f(M - mb), y = __builtin_amdgcn_exp2f(o[4] - mb);
+            A = make_float4(A.x * x + a.x * y, A.y * x + a.y * y, A.z * x + a.z * y, A.w * x + a.w * y);
+            S = S * x + o[5] * y;
+            M = mn;
+        }
+    return Joined{M, S, A};
 }
+
+// Whether this workgroup is the last of n to arrive at a counter, which is zero
+// again then.  What the workgroup wrote past the L2 can be read by the last
+// one: every wave waits until its stores are acknowledged.  (A release fence in
+// their place writes back the whole L2, 6 us a launch and more.)
+__device__ __forceinline__ bool last_of(uint32_t *counter, int n, int &flag) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const bool l = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)n - 1u;
+        if (l) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        flag = l;
+    }
+    __syncthreads();
+    return flag;
+}
+
+// A compute unit reads partials at about 35 bytes a ns, so many runs are joined
+// in groups first, by each group's last workgroup: runs of a group, 0 for none.
+// (59 runs of 4 heads at once took 6.8 us, one sequence of one kv head has 504.)
+__device__ __forceinline__ int qa_group(int ns) { return ns <= 32 ? 0 : (ns <= 64 ? 8 : (ns <= 256 ? 16 : 32)); }
 
 template <int FMT, int B, int DT, bool SEL>
 __global__ void __launch_bounds__(64 * QA_NWV) __attribute__((amdgpu_waves_per_eu(2)))
@@ -378,20 +400,28 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         }
     }
     if (pl.ns == 1) return;
-    // The pair's last workgroup joins its runs, in their order whichever it is.
-    // Partials are written and read past the XCD's L2 (agent scope): once a
-    // wave's stores are acknowledged every XCD reads them.  (A release fence in
-    // their place writes back the whole L2, 6 us a launch and more.)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-        const bool l = __hip_atomic_fetch_add(&arrivals[p], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pl.ns - 1u;
-        if (l) __hip_atomic_store(&arrivals[p], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = l;
+    // the last workgroup of a group, then of the pair, joins its runs, in their
+    // order whichever it is; partials are written and read past the XCD's L2
+    const float *first = part + (uint64_t)(blockIdx.x - pl.i) * QA_PART;
+    const int group = qa_group(pl.ns);
+    int ns = pl.ns, stride = QA_PART;
+    if (group) {
+        const int at = pl.i / group * group;
+        if (!last_of(arrivals + Q_RUNS + (blockIdx.x - pl.i + at), min(group, ns - at), last)) return;
+        const Joined j = join_runs(first + (uint64_t)at * QA_PART, QA_PART, min(group, ns - at), q.G, &mrg[0][0][0]);
+        if (tid < 32 * q.G) {                              // to the place of the group's first run
+            float *to = part + (uint64_t)(blockIdx.x - pl.i + at) * QA_PART;
+            const float a[4] = {j.A.x, j.A.y, j.A.z, j.A.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put(to + 2 * QA_HEADS + 4 * tid + e, a[e]);
+            if (tid % 32 == 0) { put(to + tid / 16, j.M); put(to + tid / 16 + 1, j.S); }
+        }
+        ns = (ns + group - 1) / group;
+        stride = group * QA_PART;
     }
-    __syncthreads();
-    if (!last) return;
-    join_runs(part + (uint64_t)(blockIdx.x - pl.i) * QA_PART, pl.ns, q.G, &mrg[0][0][0], out);
+    if (!last_of(arrivals + p, ns, last)) return;
+    const Joined j = join_runs(first, stride, ns, q.G, &mrg[0][0][0]);
+    if (tid < 32 * q.G) *(float4 *)(out + 4 * tid) = make_float4(joined(j.A.x, j.S), joined(j.A.y, j.S), joined(j.A.z, j.S), joined(j.A.w, j.S));
 }
 
 }  // namespace
@@ -401,7 +431,7 @@ hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint
                                void *ws, float *out, hipStream_t s) {
     const int pairs = q.S * q.H, runs = qa_runs(pairs) + pairs;
     uint32_t *arrivals = (uint32_t *)ws;
-    float *part = (float *)(arrivals + Q_PAIRS + 1);
+    float *part = (float *)(arrivals + 2 * Q_RUNS);
     const int units = (sel.list ? q_want(q.N, sel.num, sel.den) : q.N) + 1;
     const long long most = (long long)pairs * ceil_div(units, QA_LEAST);
     const dim3 grid((uint32_t)(most < runs ? most : runs));

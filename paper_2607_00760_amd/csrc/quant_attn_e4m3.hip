@@ -9,7 +9,7 @@ hipError_t launch_quant_attn_e4m3(const QCache &q, int block, int dtype, const u
 }
 
 size_t quant_attn_ws_bytes(int pairs) {
-    return (size_t)(Q_PAIRS + 1) * sizeof(uint32_t) + (size_t)(qa_runs(pairs) + pairs) * QA_PART * sizeof(float);
+    return (size_t)2 * Q_RUNS * sizeof(uint32_t) + (size_t)(qa_runs(pairs) + pairs) * QA_PART * sizeof(float);
 }
 
 }  // namespace mosaic

@@ -255,6 +255,23 @@ def test_uneven_batches_share_the_work(S, H):
             close(part[s, at], want, zmax, f"s={s} h={h} selected")
 
 
+@pytest.mark.parametrize("H,nb,G", [(1, 5000, 8), (1, 1500, 1), (2, 700, 5), (1, 300, 3), (1, 250, 2)])
+def test_pairs_of_many_runs(H, nb, G):
+    """Few pairs take the whole chip: their runs are joined at once up to 32, in
+    groups of 8, 16 and 32 beyond; the same every time."""
+    B, n = 32, nb * 32 + 5
+    g = torch.Generator().manual_seed(nb)
+    k, v, q = tokens(g, 1, H, n, dt=torch.bfloat16), tokens(g, 1, H, n, dt=torch.bfloat16, strong=1.0), tokens(g, 1, H * G, dt=torch.bfloat16)
+    c = make("e4m3", "bf16", B, 1, H, G, n, 0xff)
+    c.append(k.cuda(), v.cuda())
+    out = c.decode(q.cuda(), SCALE)
+    for _ in range(3):
+        assert torch.equal(c.decode(q.cuda(), SCALE), out)
+    for h in range(H):
+        want, zmax = R.Pair(k[0, h], v[0, h], "e4m3", B).attend(q[0, h * G: (h + 1) * G].float().numpy(), SCALE)
+        close(out[0, h * G: (h + 1) * G], want, zmax, f"head {h}")
+
+
 def test_codes_behind_four_gibibytes():
     """The second head's codes start behind byte 2^32 of the array."""
     B, G, cap = 64, 4, (1 << 25) + 64
