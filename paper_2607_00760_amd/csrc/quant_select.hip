@@ -38,17 +38,17 @@ __device__ __forceinline__ i32x4 pack_signed(const float (&x)[16], bool upper) {
 }
 
 // The scores of blocks [b, b1) of pair p (nb blocks), a wave's 16 from b and
-// then every `step`: emit(block, score).  QS_AHEAD steps are in flight, the
+// then every `step`: emit(block, score).  AHEAD steps are in flight, the
 // first before the query is looked at.  (Loads past the end read the last
 // block again: a branch around each would wait for those before it.)
-template <int DT, int QS_AHEAD, typename E>
+template <int DT, int AHEAD, typename E>
 __device__ __forceinline__ void score_blocks(const QCache &q, int p, int nb, const uint16_t *query, int b, int b1, int step, E emit) {
     const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
     const int8_t *bp = q.bounds + (uint64_t)p * q.N * (2 * D);
     const float *bs = q.bs + (uint64_t)p * q.N;
     if (b >= b1) return;
-    i32x4 w[QS_AHEAD][4];
-    float u[QS_AHEAD];                                     // of block 4 q4 + l16 % 4
+    i32x4 w[AHEAD][4];
+    float u[AHEAD];                                     // of block 4 q4 + l16 % 4
     auto load = [&](int s, int at) {
         const i32x4 *row = (const i32x4 *)(bp + (uint64_t)min(at + l16, nb - 1) * (2 * D)) + q4;
 #pragma unroll
@@ -56,7 +56,7 @@ __device__ __forceinline__ void score_blocks(const QCache &q, int p, int nb, con
         u[s] = bs[min(at + 4 * q4 + (l16 & 3), nb - 1)];
     };
 #pragma unroll
-    for (int s = 0; s < QS_AHEAD; ++s) load(s, b + s * step);
+    for (int s = 0; s < AHEAD; ++s) load(s, b + s * step);
     const int head = min(l16, q.G - 1);                    // columns past the group repeat its last head
     const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
     float x[2][16];
@@ -95,14 +95,14 @@ __device__ __forceinline__ void score_blocks(const QCache &q, int p, int nb, con
         const int blk = at + 4 * q4 + l16;
         if (l16 < 4 && blk < b1) emit(blk, mine * u[s]);
     };
-    for (; b + QS_AHEAD * step < b1; b += QS_AHEAD * step)
+    for (; b + AHEAD * step < b1; b += AHEAD * step)
 #pragma unroll
-        for (int s = 0; s < QS_AHEAD; ++s) {
+        for (int s = 0; s < AHEAD; ++s) {
             score(s, b + s * step);
-            load(s, b + (s + QS_AHEAD) * step);
+            load(s, b + (s + AHEAD) * step);
         }
 #pragma unroll
-    for (int s = 0; s < QS_AHEAD; ++s) score(s, b + s * step);
+    for (int s = 0; s < AHEAD; ++s) score(s, b + s * step);
 }
 
 // grid QS_RUNS + pairs: one run of 64-block units of a pair each
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const 
     float *out = scores + (uint64_t)p * q_score_stride(q.N);
     auto emit = [&](int at, float s) { out[at] = s; };
     if (pl.c == 1) score_blocks<DT, 1>(q, p, nb, query, b0 + 16 * wave, b1, QS_UNIT, emit);
-    else score_blocks<DT, 4>(q, p, nb, query, b0 + 16 * wave, b1, QS_UNIT, emit);
+    else score_blocks<DT, 2>(q, p, nb, query, b0 + 16 * wave, b1, QS_UNIT, emit);
 }
 
 // The `want` (at least one) best of a pair's scores src[0, nb), by one workgroup
