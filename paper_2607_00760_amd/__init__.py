@@ -555,12 +555,21 @@ class QuantCache:
         return {n: getattr(self, n) for n in self.TENSORS}
 
     def reset(self, seqs=None):
-        """Empties the cache, or the sequences of an index tensor or list."""
+        """Empties the cache, or the sequences of a list of indices or of an
+        integer tensor on the GPU (values outside 0..S - 1 name none)."""
         import torch
         if seqs is None:
             self.lens.zero_()
-        else:
-            self.lens[torch.as_tensor(seqs, dtype=torch.long, device=self.device)] = 0
+            return
+        if not isinstance(seqs, torch.Tensor):
+            seqs = [int(s) for s in seqs]
+            if any(not 0 <= s < self.num_seqs for s in seqs):
+                raise ValueError(f"sequences {seqs} of {self.num_seqs}")
+            seqs = torch.tensor(seqs, dtype=torch.int32, device=self.device)
+        if seqs.dtype not in (torch.int32, torch.int64) or seqs.device != self.device or seqs.dim() != 1:
+            raise ValueError("seqs must be a list of indices or a one-dimensional integer tensor on the cache's GPU")
+        named = (torch.arange(self.num_seqs, device=self.device)[:, None] == seqs).any(1)
+        self.lens.masked_fill_(named[:, None], 0)
 
     def append(self, k, v, new_lens=None):
         """k, v: [S][H][n][128] or [S][H][128] (one token), any strides with

@@ -46,11 +46,11 @@ template <int FMT> __device__ __forceinline__ uint32_t codes4(const float (&y)[4
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u), __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), 0x05040100u);
 }
 
-// grid (blocks that the call may complete, pairs).  The last of a
-// pair's workgroups to have read the length writes the new one; grids of more
-// than QN_ARRIVE blocks leave that to a launch of its own (4 us): an arrival at
-// one address takes 12 ns, and 1025 a pair of 32 took the prefill of 4 x 32785
-// tokens from 160 to 176 us (and to 388 with the pairs' counters in one line).
+// grid (blocks that the call may complete, pairs).  The last of a pair's
+// workgroups to have read the length writes the new one; grids of more than
+// QN_ARRIVE blocks leave that to a launch of its own (4 us): an arrival at one
+// address takes 12 ns, and 1025 for each of 32 pairs took the prefill of 4 x
+// 32785 tokens from 158 to 176 us (to 388 with the pairs' counters in one line).
 template <int FMT, int B, int DT>
 __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw) {
     constexpr int HW = 4 * B / 64;                             // waves of a half
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw) {
     int n = nw.counts ? nw.counts[s] : nw.max_new;
     n = min(max(n, 0), nw.max_new);
     if (n == 0) return;
-    if (n > q.cap - L) {               // no room: the sequence stays as it is
+    if (n > q.cap - L) {                                       // no room: the sequence stays as it is
         if (j == 0 && h == 0 && tid == 0) q.refused[s] += 1;
         return;
     }

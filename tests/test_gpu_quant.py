@@ -140,8 +140,14 @@ def test_append_without_room():
     same_state(c, pairs, 0xff)
     with pytest.raises(M.MosaicError):
         c.append(torch.zeros(S, H, 2 * B + 1, D, dtype=dt, device="cuda"), torch.zeros(S, H, 2 * B + 1, D, dtype=dt, device="cuda"))
-    c.reset([1])
+    c.reset([1, 1])
     assert c.lens.tolist() == [[2 * B] * H, [0] * H, [1] * H]
+    c.reset(torch.tensor([2, 7, -1], device="cuda"))
+    assert c.lens.tolist() == [[2 * B] * H, [0] * H, [0] * H]
+    for bad in ([3], [-1], torch.tensor([True, False, False], device="cuda"), torch.tensor([0])):
+        with pytest.raises(ValueError):
+            c.reset(bad)
+    assert c.lens.tolist() == [[2 * B] * H, [0] * H, [0] * H]
     c.reset()
     assert not c.lens.any()
 
