@@ -454,7 +454,7 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
         a = _rows(x, name, shape, dt, dev)
         want = (shape[0], shape[2], shape[1], D) if swap else shape
         if out is None:
-            out = torch.empty(want, dtype=dt, device=dev)
+            out = x.new_empty(want)
             b = out.stride()
         else:
             b = _rows(out, name + "_out", want, dt, dev)

@@ -56,26 +56,35 @@ template <int DT, bool INTER>
 __global__ void __launch_bounds__(256) k_norm_rope(NormRope a, int rounds) {
     __shared__ __align__(16) float cs[2][D / 2];
     const int tid = threadIdx.x, l = tid & 15, half = a.half;
-    const long long t = blockIdx.x;
-    const long long s = t / a.n, j = t - s * a.n;
-    const int nrows = a.hq + (a.v ? 2 : 1) * a.hkv, row0 = blockIdx.y * rounds * NR_ROWS + (tid >> 4);
+    const int64_t s = blockIdx.x / a.n, j = blockIdx.x % a.n;
+    const int nrows = a.hq + (a.v ? 2 : 1) * a.hkv, g = (tid & 63) >> 4;
+    const int rw0 = blockIdx.y * rounds * NR_ROWS + 4 * __builtin_amdgcn_readfirstlane(tid >> 6);    // the wave's first row
     // the lane's channels c0..c0 + 3 and c1..c1 + 3: pairs (c0 + i, c1 + i), or
     // (c0 + 2 i, c0 + 2 i + 1); lanes past the pairs hold the other channels
     const bool turned = 8 * l < 2 * half;
     const int c0 = INTER || !turned ? 8 * l : 4 * l, c1 = INTER || !turned ? 8 * l + 4 : half + 4 * l;
     uint2 x[NR_AHEAD][2];
-    int64_t to[NR_AHEAD];
+    uint16_t *to[NR_AHEAD];
+    auto kind_of = [&](int row) { return row < a.hq ? 0 : (row < a.hq + a.hkv ? 1 : 2); };
 #pragma unroll
     for (int it = 0; it < NR_AHEAD; ++it) {
-        const int row = row0 + it * NR_ROWS;
+        const int rw = rw0 + it * NR_ROWS, row = rw + g;
         if (it < rounds && row < nrows) {
-            const int kind = row < a.hq ? 0 : (row < a.hq + a.hkv ? 1 : 2);
-            const int h = kind == 0 ? row : (kind == 1 ? row - a.hq : row - a.hq - a.hkv);
-            const NormRope::Part &p = kind == 0 ? a.q : (kind == 1 ? a.k : a.vp);
-            const uint16_t *src = p.in + s * p.in_seq + j * p.in_tok + h * p.in_head;
+            const uint16_t *src;
+            const int kw = kind_of(rw);
+            if (kw == kind_of(rw + 3)) {                   // the wave's rows are heads of one kind: scalar addresses, and a
+                const NormRope::Part &p = kw == 0 ? a.q : (kw == 1 ? a.k : a.vp);      // lane's head in steps of two strides
+                const int h = rw - (kw == 0 ? 0 : (kw == 1 ? a.hq : a.hq + a.hkv));
+                src = p.in + (s * p.in_seq + j * p.in_tok + h * p.in_head) + ((g & 1) ? p.in_head : 0) + ((g & 2) ? 2 * p.in_head : 0);
+                to[it] = p.out + (s * p.out_seq + j * p.out_tok + h * p.out_head) + ((g & 1) ? p.out_head : 0) + ((g & 2) ? 2 * p.out_head : 0);
+            } else {
+                const int kind = kind_of(row), h = row - (kind == 0 ? 0 : (kind == 1 ? a.hq : a.hq + a.hkv));
+                const NormRope::Part &p = kind == 0 ? a.q : (kind == 1 ? a.k : a.vp);
+                src = p.in + s * p.in_seq + j * p.in_tok + h * p.in_head;
+                to[it] = p.out + s * p.out_seq + j * p.out_tok + h * p.out_head;
+            }
             x[it][0] = *(const uint2 *)(src + c0);
             x[it][1] = *(const uint2 *)(src + c1);
-            to[it] = s * p.out_seq + j * p.out_tok + h * p.out_head;
         }
     }
     if (tid < half) {
@@ -147,20 +156,13 @@ __global__ void __launch_bounds__(256) k_norm_rope(NormRope a, int rounds) {
     };
 #pragma unroll
     for (int it = 0; it < NR_AHEAD; ++it) {
-        const int row = row0 + it * NR_ROWS;
+        const int row = rw0 + it * NR_ROWS + g;
         if (it < rounds && row < nrows) {
-            uint16_t *dst = a.q.out;
-            if (row < a.hq) {
-                rotate(x[it], turn[0]);
-            } else if (row < a.hq + a.hkv) {
-                rotate(x[it], turn[1]);
-                dst = a.k.out;
-            } else {
-                dst = a.vp.out;
-            }
+            if (row < a.hq) rotate(x[it], turn[0]);
+            else if (row < a.hq + a.hkv) rotate(x[it], turn[1]);
             // (streamed: 32768 tokens of 48 rows 173 us without, 167 with)
-            __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, x[it][0]), (uint64_t *)(dst + to[it] + c0));
-            __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, x[it][1]), (uint64_t *)(dst + to[it] + c1));
+            __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, x[it][0]), (uint64_t *)(to[it] + c0));
+            __builtin_nontemporal_store(__builtin_bit_cast(uint64_t, x[it][1]), (uint64_t *)(to[it] + c1));
         }
     }
 }
