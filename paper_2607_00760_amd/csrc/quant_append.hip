@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw) {
         if (!vals) {
             uint8_t *kp = q.k + blk * (B * D);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) *(uint2 *)(kp + (4 * t4 + r) * D + 8 * pc) = make_uint2(c[r][0], c[r][1]);
+            for (int r = 0; r < 4; ++r)                        // (streamed: 148 -> 145 us; the values' 4-byte pieces gain nothing)
+                __builtin_nontemporal_store((uint64_t)c[r][1] << 32 | c[r][0], (uint64_t *)(kp + (4 * t4 + r) * D + 8 * pc));
             if (tid < D / 2) {                                 // two channels each
                 const float unit = 127.0f / a;
                 const int g = tid >> 2, d = tid & 3;
