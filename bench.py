@@ -115,8 +115,8 @@ def algorithmic_bytes(cache, spec, nb_list, sel_list, desc_list):
 
 
 # sources of the other paths' kernels; every other file of csrc takes part in the decode step
-OTHER_SOURCES = ("compress.hip", "dense.hip", "encode.hip", "norm_rope.hip", "quant.h", "quant_api.hip", "quant_append.hip",
-                 "quant_attn.h", "quant_attn_e4m3.hip", "quant_attn_int8.hip", "quant_select.hip", "rotation.hip")
+OTHER_SOURCES = ("compress.hip", "dense.hip", "encode.hip", "norm_rope.h", "norm_rope.hip", "quant.h", "quant_api.hip",
+                 "quant_append.hip", "quant_attn.h", "quant_attn_e4m3.hip", "quant_attn_int8.hip", "quant_select.hip", "rotation.hip")
 
 
 def source_hash():

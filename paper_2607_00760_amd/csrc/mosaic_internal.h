@@ -290,19 +290,6 @@ hipError_t launch_dense(const uint16_t *q, const uint16_t *k, const uint16_t *v,
                         int hkv, int G, int dtype, int64_t seq_stride, int max_ctx, const int32_t *ctx,
                         float scale, float *part, hipStream_t s);
 
-// queries, keys and (v set) values of `seqs` sequences of n tokens
-struct NormRope {
-    struct Part { const uint16_t *in; uint16_t *out; int64_t in_seq, in_tok, in_head, out_seq, out_tok, out_head; };
-    Part q, k, vp;
-    const uint16_t *qw, *kw;              // weights, or null: no norm
-    const float *inv_freq;                // [half]
-    const void *pos;
-    int64_t pos_seq, pos_tok;
-    int seqs, n, hq, hkv, half, pos64, v;
-    float eps;
-};
-hipError_t launch_norm_rope(const NormRope &a, int dtype, int interleaved, hipStream_t s);
-
 size_t dense_part_bytes(int npairs, int G, int max_ctx);
 size_t rotation_ctx_bytes(int num_seqs);
 size_t rotation_ws_bytes(int num_seqs, int hkv, int nw, int W);

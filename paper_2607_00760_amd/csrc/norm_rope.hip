@@ -15,7 +15,7 @@
 // cosines are made once, and a pair costs six multiplications.  64 lanes
 // compute the token's angles while the rows are on their way.  HBM is the
 // bound: every row is read and written once.
-#include "mosaic_internal.h"
+#include "norm_rope.h"
 
 namespace mosaic {
 

@@ -5,6 +5,7 @@
 #include <cstdio>
 
 #include "../../include/mosaic.h"
+#include "norm_rope.h"
 #include "quant.h"
 
 using namespace mosaic;
