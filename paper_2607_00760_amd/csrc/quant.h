@@ -34,42 +34,47 @@ struct QNew {                                              // tokens to append, 
     int max_new;
 };
 
-// How a launch of about `slots` workgroups shares the units of all pairs: runs
-// of c >= cmin units, c a multiple of step, that do not cross pairs.  The lengths are
-// read on the device, so a captured launch follows them; runs are equal
+// How a launch shares the units of all pairs: in runs of c units that do not
+// cross pairs, c the least that makes about `slots` runs, a multiple of step
+// and at least cmin; from there up to 2 cmin for about `few` runs.  The lengths
+// are read on the device, so a captured launch follows them; runs are equal
 // however ragged the batch, and there are at most slots + pairs of them.
+struct QShare {
+    int slots, few, cmin, step;
+    int least;                                             // runs of a pair at least
+    int alone;                                             // units that a pair's only run may have, whatever c is
+};
 struct QPlan {
     int s, h, i, ns;                                       // sequence, kv head, run of the pair, runs of the pair
     int c, L;                                              // units of a run, the sequence's tokens
     bool live;
 };
 
-// units(L): units of a pair of L tokens; least: runs of a pair at least; alone:
-// units that a pair's only run may have, whatever c is.
+// The plan of run w; units(L): units of a pair of L tokens.
 template <typename U>
-__device__ __forceinline__ QPlan q_plan(const QCache &q, int slots, int cmin, int step, int least, int alone, U units, int w) {
+__device__ __forceinline__ QPlan q_plan(const QCache &q, const QShare &sh, U units, int w) {
     const int lane = threadIdx.x & 63;
     auto length = [&](int s) { return s < q.S ? q.len((long long)s * q.H) : 0; };
     const int L0 = length(lane);
     uint32_t total = lane < q.S ? (uint32_t)units(L0) : 0u;
     for (int s = lane + 64; s < q.S; s += 64) total += (uint32_t)units(length(s));
     total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(total), 63) * (uint32_t)q.H;
-    const uint32_t c0 = (total + (uint32_t)slots - 1u) / (uint32_t)slots;
-    const int c = max(cmin, (int)((c0 + (uint32_t)step - 1u) / (uint32_t)step) * step);
+    auto runs_of = [&](int n) { return (int)((total + (uint32_t)(n * sh.step) - 1u) / (uint32_t)(n * sh.step)) * sh.step; };
+    const int c = max(max(sh.cmin, min(2 * sh.cmin, runs_of(sh.few))), runs_of(sh.slots));
     QPlan p{};
     p.c = c;
     uint32_t base = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
         const int s = s0 + lane, L = s0 ? length(s) : L0;
         const int u = s < q.S ? units(L) : 0;
-        const int ns = s < q.S ? max(least, u <= alone ? min(u, 1) : (u + c - 1) / c) : 0;
+        const int ns = s < q.S ? max(sh.least, u <= sh.alone ? min(u, 1) : (u + c - 1) / c) : 0;
         const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
         const uint64_t hit = __ballot(base + inc > (uint32_t)w);       // the first sequence whose runs end past w
         if (hit) {
             const int l = (int)__builtin_ctzll(hit);
             p.s = s0 + l;
             p.ns = __builtin_amdgcn_readlane(ns, l);
-            if (p.ns == 1) p.c = max(c, alone);
+            if (p.ns == 1) p.c = max(c, sh.alone);
             p.L = __builtin_amdgcn_readlane(L, l);
             const int r = w - ((int)(base + (uint32_t)__builtin_amdgcn_readlane((int)inc, l)) - p.ns * q.H);
             p.h = r / p.ns;

@@ -71,8 +71,8 @@ template <int FMT> __device__ __forceinline__ uint32_t codes4(const float (&y)[4
 // grid (blocks that the call may complete, pairs).  The last of a pair's
 // workgroups to have read the length writes the new one; grids of more than
 // QN_ARRIVE blocks leave that to a launch of its own (4 us): an arrival at one
-// address takes 12 ns, and 1025 for each of 32 pairs took the prefill of 4 x
-// 32785 tokens from 158 to 176 us (to 388 with the pairs' counters in one line).
+// address takes 12 ns, and 1025 for each of 32 pairs take the prefill of 4 x
+// 32785 tokens from 144 to 166 us (to 388 with the pairs' counters in one line).
 template <int FMT, int B, int DT>
 __global__ void __launch_bounds__(8 * B) k_quant_append(QCache q, QNew nw) {
     constexpr int HW = 4 * B / 64;                             // waves of a half

@@ -29,10 +29,16 @@ constexpr int QA_NWV = 4;                                  // waves of a workgro
 // Runs of a launch: with up to 256 pairs they and the pairs' rounding fill the
 // 512 workgroups that the chip holds once; more pairs take several rounds anyway.
 __host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256 ? 512 - pairs : 1024; }
-// Blocks of a run at least: two steps a wave.  1 x 4117 tokens, 8 kv heads: 4
-// blocks 11.5 us, 8 9.6, 16 11.7 (a step costs less than joining twice the runs).
-constexpr int QA_LEAST = 2 * QA_NWV;
-constexpr int QA_ALONE = 16;                               // units of a pair that one run takes: joining costs 3 us
+// Units of a run at least: two steps a wave, and up to four rather than a
+// second workgroup on a compute unit (a step costs 0.8 us, joining a pair's
+// runs 3).  us with runs of 4 / 8 / 12 / 16 units, 8 kv heads:
+//   1 x 1500 tokens            - /  8.8 /  9.4 / 10.3
+//   1 x 4117                12.5 /  9.9 /  9.5 /  9.7
+//   8 x 1500                   - / 12.3 / 11.1 / 11.6
+//   a tenth of 4 x 32785       - / 22.4 / 22.9 / 20.5
+constexpr int QA_LEAST = 2 * QA_NWV, QA_FEW = 256;
+// A pair of up to 16 units is one run: 380 tokens 8.4 -> 7.4 us.
+constexpr int QA_ALONE = 16;
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and accumulators of the heads
 
@@ -151,7 +157,8 @@ __device__ __forceinline__ bool last_of(uint32_t *counter, int n, int &flag) {
 
 // A compute unit reads partials at about 35 bytes a ns, so many runs are joined
 // in groups first, by each group's last workgroup: runs of a group, 0 for none.
-// (59 runs of 4 heads at once took 6.8 us, one sequence of one kv head has 504.)
+// (59 runs of 4 heads at once took 6.8 us; one sequence of one kv head has up to
+// 504: 256 K tokens 38.4 us at once, 21.2 in groups.)
 __device__ __forceinline__ int qa_group(int ns) { return ns <= 32 ? 0 : (ns <= 64 ? 8 : (ns <= 256 ? 16 : 32)); }
 
 template <int FMT, int B, int DT, bool SEL>
@@ -164,7 +171,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     __shared__ int last;
     auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
     auto units = [&](int L) { return blocks(L) + (L % B != 0); };        // the unfinished block is a pair's last unit
-    const QPlan pl = q_plan(q, qa_runs(q.S * q.H), QA_LEAST, QA_NWV, 1, QA_ALONE, units, blockIdx.x);
+    const QPlan pl = q_plan(q, QShare{qa_runs(q.S * q.H), QA_FEW, QA_LEAST, QA_NWV, 1, QA_ALONE}, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

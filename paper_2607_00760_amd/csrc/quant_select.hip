@@ -108,7 +108,7 @@ __device__ __forceinline__ void score_blocks(const QCache &q, int p, int nb, con
 // grid QS_RUNS + pairs: one run of 64-block units of a pair each
 template <int DT>
 __global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores, int32_t *list) {
-    const QPlan pl = q_plan(q, QS_RUNS, 1, 1, 0, 0, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
+    const QPlan pl = q_plan(q, QShare{QS_RUNS, QS_RUNS, 1, 1, 0, 0}, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
     if (!pl.live) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int p = pl.s * q.H + pl.h, nb = pl.L / block;
@@ -249,9 +249,9 @@ __global__ void __launch_bounds__(1024) k_quant_topk(QCache q, int block, int nu
 // ns at most, whoever asks: so for caches of up to 256 blocks a pair, and for
 // larger ones where there are pairs for half of the chip.  Whole calls, blocks
 // of 32, 8 kv heads, us in one workgroup / spread over several:
-//   tokens       2048         8192         16384        32768
-//   1 sequence   13.3 / 14.7  16.2 / 17.4  17.9 / 17.4  22.2 / 18.1
-//   16           13.3 / 14.9  20.6 / 22.6  26.7 / 28.7  45.2 / 48.7
+//   tokens         2048         8192         16384        32768
+//   1 sequence     13.0 / 14.6  16.2 / 17.5  18.0 / 17.4  22.3 / 18.2
+//   32             13.8 / 15.4  20.7 / 23.5  35.3 / 37.6  59.9 / 63.3
 constexpr int QK_FUSED = 1024, QK_NW = 4;
 template <int DT>
 __global__ void __launch_bounds__(64 * QK_NW) k_quant_pick(QCache q, int block, const uint16_t *query, int num, int den, int32_t *list) {
