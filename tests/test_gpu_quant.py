@@ -152,6 +152,41 @@ def test_append_without_room():
     assert not c.lens.any()
 
 
+def test_long_append_without_room():
+    """The same where a call's blocks are many and the lengths follow in a launch
+    of their own; a sequence with nothing to take beside them."""
+    B, S, H, dt, n = 32, 3, 2, torch.bfloat16, 40 * 32 + 3
+    g = torch.Generator().manual_seed(6)
+    k, v = tokens(g, S, H, n, dt=dt), tokens(g, S, H, n, dt=dt)
+    c = make("int8", "bf16", B, S, H, 1, 64 * B, 0xff)
+    counts = torch.tensor([n, 0, n - 7], dtype=torch.int32, device="cuda")
+    c.append(k.cuda(), v.cuda(), counts)
+    c.append(k.cuda(), v.cuda(), torch.tensor([n, n, 64 * B - n + 8], dtype=torch.int32, device="cuda"))
+    assert c.refused.tolist() == [1, 0, 1] and c.lens.tolist() == [[n] * H, [n] * H, [n - 7] * H]
+    same_state(c, {(s, h): R.Pair(k[s, h, : n - 7 * (s == 2)], v[s, h, : n - 7 * (s == 2)], "int8", B) for s in range(S) for h in range(H)}, 0xff)
+
+
+def test_two_caches_on_two_streams():
+    """Calls on different caches overlap; each has a workspace of its own."""
+    B, H, G, n, dt = 32, 2, 4, 9000, torch.float16
+    g = torch.Generator().manual_seed(12)
+    k, v, q = tokens(g, 1, H, n, dt=dt).cuda(), tokens(g, 1, H, n, dt=dt).cuda(), tokens(g, 1, H * G, dt=dt).cuda()
+    caches = [make("e4m3", "fp16", B, 1, H, G, n, 0xff) for _ in range(2)]
+    for c in caches:
+        c.append(k, v)
+    want = caches[0].decode(q, SCALE), caches[0].decode_selected(q, SCALE, (1, 5))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in caches], [[], []]
+    for _ in range(20):
+        for i, c in enumerate(caches):
+            with torch.cuda.stream(streams[i]):
+                got[i].append((c.decode(q, SCALE), c.decode_selected(q, SCALE, (1, 5))))
+    torch.cuda.synchronize()
+    for outs in got:
+        for a, b in outs:
+            assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
 def edges(block):
     return [0, 1, block - 1, block, block + 1, 4 * block, 5 * block + block // 2, 9 * block - 1, 17 * block + 3]
 
@@ -215,11 +250,11 @@ def test_decode_scales_that_differ(fmt, dtype, block):
 
 def test_selection_ties_and_many_blocks():
     """Equal blocks are taken from the lowest on; a pair of more blocks than a
-    workgroup has threads, and of as many different scores; both forms of the
-    selection's keys (in registers, and read again)."""
+    workgroup has threads, and of as many different scores; every form of the
+    selection (by the cache's room: keys in registers, or read again)."""
     B, G = 32, 3
     g = torch.Generator().manual_seed(2)
-    for nb, cap in ((2500, 2500), (4200, 4200), (40, 40 * 1024)):
+    for nb, cap in ((2500, 2500), (4200, 4200), (40, 40 * 1024), (700, 20 * 1024), (300, 900)):
         n = nb * B + 7
         k = tokens(g, 2, 1, n, dt=torch.bfloat16)
         k[0, 0, : nb * B] = k[0, 0, :B].repeat(nb, 1)          # sequence 0: every block the same
@@ -239,19 +274,19 @@ def test_selection_ties_and_many_blocks():
             close(out[s], want, zmax, f"{nb} blocks, sequence {s}")
 
 
-@pytest.mark.parametrize("S,H", [(70, 1), (130, 3), (3, 8)])
-def test_uneven_batches_share_the_work(S, H):
+@pytest.mark.parametrize("S,H,long", [(70, 1, 6000), (130, 3, 6000), (3, 8, 6000), (129, 1, 11000), (300, 1, 900)])
+def test_uneven_batches_share_the_work(S, H, long):
     """Many short sequences, empty ones and long ones: the runs of every pair
     are found and joined."""
     B, G, dt = 32, 2, torch.float16
-    lens = [0 if s % 9 == 4 else (6000 + s if s in (1, S - 1) else 5 * s % 97) for s in range(S)]
+    lens = [0 if s % 9 == 4 else (long + s if s in (1, S - 1) else 5 * s % 97) for s in range(S)]
     g = torch.Generator(device="cuda").manual_seed(S)
     k, v = (torch.randn(S, H, max(lens), D, generator=g, device="cuda").to(dt) for _ in range(2))
     q = torch.randn(S, H * G, D, generator=g, device="cuda").to(dt)
     c = make("int8", "fp16", B, S, H, G, max(lens), 0xff)
     c.append(k, v, torch.tensor(lens, dtype=torch.int32, device="cuda"))
     out, part = c.decode(q, SCALE), c.decode_selected(q, SCALE, (1, 5))
-    for s in [s for s in range(S) if lens[s] > 1000 or s % 13 == 0 or s % 9 == 4]:
+    for s in [s for s in range(S) if lens[s] > 800 or s % 13 == 0 or s % 9 == 4]:
         for h in range(H):
             r = R.Pair(k[s, h, : lens[s]].cpu(), v[s, h, : lens[s]].cpu(), "int8", B)
             qs, at = q[s, h * G: (h + 1) * G].float().cpu().numpy(), slice(h * G, (h + 1) * G)
