@@ -529,7 +529,7 @@ mosaic_status mosaic_quant_workspace_bytes(const mosaic_quant_cache *cache, size
 /* Decode attention over every token of the cache (dequantised codes, and the
  * tail), one query token a sequence.
  *   q   : [S][H * group_size][128] (cache dtype), 16-byte aligned
- *   out : [S][H * group_size][128] fp32
+ *   out : [S][H * group_size][128] fp32, 16-byte aligned
  *   ws  : at least mosaic_quant_workspace_bytes bytes, 256-byte aligned
  * A sequence without tokens gets zeros.  Logits must stay within fp32. */
 mosaic_status mosaic_quant_decode_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,

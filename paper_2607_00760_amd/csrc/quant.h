@@ -43,6 +43,8 @@ struct QShare {
     int slots, few, cmin, step;
     int least;                                             // runs of a pair at least
     int alone;                                             // units that a pair's only run may have, whatever c is
+    int join;                                              // runs that are joined in one go: pairs of up to join * 2 cmin
+                                                           // units have no more
 };
 struct QPlan {
     int s, h, i, ns;                                       // sequence, kv head, run of the pair, runs of the pair
@@ -62,19 +64,20 @@ __device__ __forceinline__ QPlan q_plan(const QCache &q, const QShare &sh, U uni
     auto runs_of = [&](int n) { return (int)((total + (uint32_t)(n * sh.step) - 1u) / (uint32_t)(n * sh.step)) * sh.step; };
     const int c = max(max(sh.cmin, min(2 * sh.cmin, runs_of(sh.few))), runs_of(sh.slots));
     QPlan p{};
-    p.c = c;
     uint32_t base = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
         const int s = s0 + lane, L = s0 ? length(s) : L0;
         const int u = s < q.S ? units(L) : 0;
-        const int ns = s < q.S ? max(sh.least, u <= sh.alone ? min(u, 1) : (u + c - 1) / c) : 0;
+        int cu = u <= sh.alone ? max(c, sh.alone) : c;
+        if (u > sh.join * c && u <= sh.join * 2 * sh.cmin) cu = (u + sh.join * sh.step - 1) / (sh.join * sh.step) * sh.step;
+        const int ns = s < q.S ? max(sh.least, (u + cu - 1) / cu) : 0;
         const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
         const uint64_t hit = __ballot(base + inc > (uint32_t)w);       // the first sequence whose runs end past w
         if (hit) {
             const int l = (int)__builtin_ctzll(hit);
             p.s = s0 + l;
             p.ns = __builtin_amdgcn_readlane(ns, l);
-            if (p.ns == 1) p.c = max(c, sh.alone);
+            p.c = __builtin_amdgcn_readlane(cu, l);
             p.L = __builtin_amdgcn_readlane(L, l);
             const int r = w - ((int)(base + (uint32_t)__builtin_amdgcn_readlane((int)inc, l)) - p.ns * q.H);
             p.h = r / p.ns;

@@ -79,8 +79,8 @@ mosaic_status attend_args(const mosaic_quant_cache *c, const void *q, const floa
     const mosaic_status st = quant_arrays(c, qc);
     if (st != MOSAIC_OK) return st;
     if (!q || !out || !ws) return fail(MOSAIC_ERR_INVALID, "NULL argument");
-    if (off16(q) || (uintptr_t)out % 4 || (uintptr_t)ws % 256)
-        return fail(MOSAIC_ERR_INVALID, "q must be 16-byte, out 4-byte, the workspace 256-byte aligned");
+    if (off16(q) || off16(out) || (uintptr_t)ws % 256)
+        return fail(MOSAIC_ERR_INVALID, "q and out must be 16-byte, the workspace 256-byte aligned");
     const uint64_t need = quant_ws(c).total;
     if (ws_bytes < need) return fail(MOSAIC_ERR_INVALID, "workspace %zu < %llu", ws_bytes, (unsigned long long)need);
     return MOSAIC_OK;

@@ -33,12 +33,14 @@ __host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256
 // second workgroup on a compute unit (a step costs 0.8 us, joining a pair's
 // runs 3).  us with runs of 4 / 8 / 12 / 16 units, 8 kv heads:
 //   1 x 1500 tokens            - /  8.8 /  9.4 / 10.3
-//   1 x 4117                12.5 /  9.9 /  9.5 /  9.7
+//   1 x 4117                12.5 /  9.9 /  9.5 /  9.7  (before QA_JOIN)
 //   8 x 1500                   - / 12.3 / 11.1 / 11.6
 //   a tenth of 4 x 32785       - / 22.4 / 22.9 / 20.5
 constexpr int QA_LEAST = 2 * QA_NWV, QA_FEW = 256;
-// A pair of up to 16 units is one run: 380 tokens 8.4 -> 7.4 us.
-constexpr int QA_ALONE = 16;
+// A pair of up to 16 units is one run: 380 tokens 8.4 -> 7.4 us.  Pairs of up to
+// 256 have no more runs than are joined with one round of loads (groups of up to
+// 4 heads): 1 x 4117 tokens 9.7 -> 9.3.
+constexpr int QA_ALONE = 16, QA_JOIN = 16;
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and accumulators of the heads
 
@@ -73,7 +75,9 @@ template <int FMT, int B> struct QStage {                  // a block in flight
 __device__ __forceinline__ float joined(float a, float s) { return s > 0.0f ? a / s : (s != s ? s : 0.0f); }
 
 // partials, past the XCD's L2
-__device__ __forceinline__ void put(float *p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void put2(float *p, float2 x) {
+    __hip_atomic_store((uint64_t *)p, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ float2 get2(const float *p) {
     return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
@@ -171,7 +175,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     __shared__ int last;
     auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
     auto units = [&](int L) { return blocks(L) + (L % B != 0); };        // the unfinished block is a pair's last unit
-    const QPlan pl = q_plan(q, QShare{qa_runs(q.S * q.H), QA_FEW, QA_LEAST, QA_NWV, 1, QA_ALONE}, units, blockIdx.x);
+    const QPlan pl = q_plan(q, QShare{qa_runs(q.S * q.H), QA_FEW, QA_LEAST, QA_NWV, 1, QA_ALONE, QA_JOIN}, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -387,23 +391,26 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     float *out = outp + (uint64_t)p * q.G * D;
     // partials of a pair's runs are consecutive: run 0's is this workgroup's less pl.i
     float *mine = part + (uint64_t)blockIdx.x * QA_PART;
-    for (int i = tid; i < q.G * D; i += 64 * QA_NWV) {
+    for (int i = 2 * tid; i < q.G * D; i += 128 * QA_NWV) {    // two columns of a head
         const int h = i / D, c = i % D;
-        float M = -INFINITY;
+        float m[QA_NWV], M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < QA_NWV; ++w) M = fmaxf(M, mrg[w][h][0]);
-        float A = 0.0f, S = 0.0f;
+        for (int w = 0; w < QA_NWV; ++w) { m[w] = mrg[w][h][0]; M = fmaxf(M, m[w]); }
+        float2 A = make_float2(0.0f, 0.0f);
+        float S = 0.0f;
 #pragma unroll
         for (int w = 0; w < QA_NWV; ++w) {
-            const float f = mrg[w][h][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mrg[w][h][0] - M);
-            A += (mrg[w][h][2 + c] + mrg[w][h + 8][2 + c]) * f;
+            const float f = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[w] - M);
+            const float2 u = *(const float2 *)&mrg[w][h][2 + c], v = *(const float2 *)&mrg[w][h + 8][2 + c];
+            A.x += (u.x + v.x) * f;
+            A.y += (u.y + v.y) * f;
             S += mrg[w][h][1] * f;
         }
         if (pl.ns == 1) {
-            out[i] = joined(A, S);
+            *(float2 *)(out + i) = make_float2(joined(A.x, S), joined(A.y, S));
         } else {
-            put(mine + 2 * QA_HEADS + i, A);
-            if (c == 0) { put(mine + 2 * h, M); put(mine + 2 * h + 1, S); }
+            put2(mine + 2 * QA_HEADS + i, A);
+            if (c == 0) put2(mine + 2 * h, make_float2(M, S));
         }
     }
     if (pl.ns == 1) return;
@@ -418,10 +425,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         const Joined j = join_runs(first + (uint64_t)at * QA_PART, QA_PART, min(group, ns - at), q.G, &mrg[0][0][0]);
         if (tid < 32 * q.G) {                              // to the place of the group's first run
             float *to = part + (uint64_t)(blockIdx.x - pl.i + at) * QA_PART;
-            const float a[4] = {j.A.x, j.A.y, j.A.z, j.A.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) put(to + 2 * QA_HEADS + 4 * tid + e, a[e]);
-            if (tid % 32 == 0) { put(to + tid / 16, j.M); put(to + tid / 16 + 1, j.S); }
+            put2(to + 2 * QA_HEADS + 4 * tid, make_float2(j.A.x, j.A.y));
+            put2(to + 2 * QA_HEADS + 4 * tid + 2, make_float2(j.A.z, j.A.w));
+            if (tid % 32 == 0) put2(to + tid / 16, make_float2(j.M, j.S));
         }
         ns = (ns + group - 1) / group;
         stride = group * QA_PART;

@@ -81,7 +81,7 @@ def test_arguments_that_are_refused(lib):
     refused(lib, CAPACITY, lambda: append(lib, c, n=3201))
     refused(lib, UNSUPPORTED, lambda: append(lib, c, n=1 << 28, lens=FAKE))
     for call in (decode, select):
-        for kw in (dict(q=None), dict(out=None), dict(ws=None), dict(q=FAKE + 8), dict(out=FAKE + 2), dict(ws=FAKE + 16),
+        for kw in (dict(q=None), dict(out=None), dict(ws=None), dict(q=FAKE + 8), dict(out=FAKE + 8), dict(ws=FAKE + 16),
                    dict(nbytes=n.value - 1)):
             refused(lib, INVALID, lambda: call(lib, c, **kw))
     for kw in (dict(num=0), dict(num=2, den=1), dict(den=0), dict(num=-1, den=-1), dict(blocks=FAKE + 1)):
