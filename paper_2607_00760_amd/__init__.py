@@ -412,6 +412,14 @@ def _rows(t, name, shape, dtype, device):
     return st
 
 
+def _vector(t, name, dtype, device):
+    """Checks a vector; returns its length."""
+    _check_tensor(t, name, dtype, device)
+    if t.dim() != 1:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected one dimension")
+    return t.shape[0]
+
+
 def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, v=None,
                  q_out=None, k_out=None, v_out=None):
     """Norm of each query and key head (with weights) and rotation to the
@@ -443,11 +451,12 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
         raise ValueError(f"positions: shape {tuple(positions.shape)} on {positions.device}, expected {(S, n)} on {dev}")
     if (q_weight is None) != (k_weight is None):
         raise ValueError("give both weights or neither")
-    for w, name, size, wdt in ((inv_freq, "inv_freq", None, torch.float32), (q_weight, "q_weight", (D,), dt), (k_weight, "k_weight", (D,), dt)):
-        if w is not None or size is None:
-            _check_tensor(w, name, wdt, dev)
-            if w.dim() != 1 or (size and w.shape != size):
-                raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {size or '(R / 2,)'}")
+    half = _vector(inv_freq, "inv_freq", torch.float32, dev)
+    qw = kw = None
+    if q_weight is not None:
+        if _vector(q_weight, "q_weight", dt, dev) != D or _vector(k_weight, "k_weight", dt, dev) != D:
+            raise ValueError(f"weights of {tuple(q_weight.shape)} and {tuple(k_weight.shape)}, expected {(D,)}")
+        qw, kw = q_weight.data_ptr(), k_weight.data_ptr()
 
     def rows(x, out, name, shape, swap):
         """x's rows and its output's ([S][Hkv][n][128] where swap is set)."""
@@ -469,9 +478,8 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
         raise ValueError("v_out without v")
     if S and n:
         _launch(dev, load().mosaic_qk_norm_rope, q_rows, k_rows, v_rows, S, n, hq, hkv, D, 1 if dt == torch.bfloat16 else 0,
-                None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
-                positions.data_ptr(), positions.element_size(), _pack2(*positions.stride()), inv_freq.data_ptr(),
-                2 * inv_freq.numel(), int(interleaved))
+                qw, kw, eps, positions.data_ptr(), positions.element_size(), _pack2(*positions.stride()), inv_freq.data_ptr(),
+                2 * half, int(interleaved))
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 

@@ -248,6 +248,31 @@ def test_decode_scales_that_differ(fmt, dtype, block):
         close(out[0, h: h + 1], want, zmax, f"head {h}")
 
 
+@pytest.mark.parametrize("fmt,dtype,block", FORMS)
+def test_values_that_are_not_finite_stay_in_their_head(fmt, dtype, block):
+    """An infinity or a NaN in a whole block or in the unfinished one spoils its
+    own (sequence, kv head); the others are as without it, bit for bit."""
+    B, H, G, dt = block, 2, 3, DT[dtype]
+    n = 20 * B + 7
+    g = torch.Generator().manual_seed(15)
+    k, v, q = tokens(g, 4, H, n, dt=dt), tokens(g, 4, H, n, dt=dt), tokens(g, 4, H * G, dt=dt, strong=1.0)
+    bad_k, bad_v = k.clone(), v.clone()
+    bad_k[0, 0, 3 * B + 1, 7] = float("inf")
+    bad_v[0, 1, 5 * B + 9, 100] = float("nan")
+    bad_k[1, 0, n - 2, 3] = float("nan")
+    bad_v[1, 1, n - 1, 0] = -float("inf")
+    outs = []
+    for kk, vv in ((k, v), (bad_k, bad_v)):
+        c = make(fmt, dtype, B, 4, H, G, n, 0xff)
+        c.append(kk.cuda(), vv.cuda())
+        outs.append((c.decode(q.cuda(), SCALE), c.decode_selected(q.cuda(), SCALE, (1, 4))))
+    for clean, spoilt in zip(*outs):
+        assert torch.equal(clean[2:], spoilt[2:]) and torch.isfinite(clean).all()
+    for s in range(2):
+        for h in range(H):
+            assert not torch.isfinite(outs[1][0][s, h * G: (h + 1) * G]).all()
+
+
 def test_selection_ties_and_many_blocks():
     """Equal blocks are taken from the lowest on; a pair of more blocks than a
     workgroup has threads, and of as many different scores; every form of the
