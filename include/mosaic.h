@@ -488,8 +488,8 @@ mosaic_status mosaic_qk_norm_rope(const mosaic_rows *q, const mosaic_rows *k, co
  * num_kv_heads, N = max_blocks, B = block_len (32 or 64); room is N B tokens a
  * sequence.  lens must start at zero; setting a sequence's entries to zero (or
  * all of them) empties it.  What lies behind a sequence's last block or token
- * is never read and left as it was.  K and V must be finite; a value that is
- * not spoils its own (sequence, kv head) only. */
+ * takes part in nothing, whatever it holds, and is left as it was.  K and V must
+ * be finite; a value that is not spoils its own (sequence, kv head) only. */
 typedef enum { MOSAIC_E4M3 = 0, MOSAIC_INT8 = 1 } mosaic_code_format;
 typedef struct {
     int32_t num_seqs, num_kv_heads, group_size, head_dim;  /* head_dim 128, group_size 1..8 */

@@ -1,5 +1,5 @@
 // quant.h -- shared by the kernels of the 8-bit KV cache (quant_append.hip,
-// quant_attn.hip, quant_select.hip) and by their entry points (quant_api.hip)
+// quant_attn.h, quant_select.hip) and by their entry points (quant_api.hip)
 // (not part of the C ABI).
 #pragma once
 #include "decode_common.h"
