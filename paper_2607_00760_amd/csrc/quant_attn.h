@@ -257,7 +257,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         const float mb = mn == -INFINITY ? 0.0f : mn;
         const float alpha = __builtin_amdgcn_exp2f(m_run - mb);
         float ls = 0.0f;
-        const float wf = ref > 0.0f ? vs * (PS / ref) : 0.0f;
+        const float wf = ref > 0.0f ? vs * (PS / ref) : vs;    // (no scale above zero yet: vs is not finite, and stays so)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
