@@ -9,7 +9,9 @@
 // a query of 8 or 11 bits too (bf16 after a power of two per head), and the
 // weights take part as two fp16 parts, 22 bits, in rows 0..7 and 8..15 of the
 // left operand, which groups of up to 8 heads leave room for.  A block's value
-// scale goes into its weights, relative to the largest scale so far.
+// scale goes into its weights; the unit of a head's sums is a power of two that
+// follows the largest product of weight and scale, so that a block is as exact
+// as its share of the output asks, however far apart the scales are.
 //
 // The products' layouts ask for 8 tokens of one channel in a lane: values lie
 // by channel in the cache, and the rows of the first product are dealt so that
@@ -170,7 +172,10 @@ __global__ void __launch_bounds__(64 * QA_NWV) __attribute__((amdgpu_waves_per_e
 k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *arrivals, float *part, float *outp) {
     using DM = DMma<DT>;
     constexpr int NT = B / 16, TPQ = B / 4;                // tiles of 16 tokens, tokens of a lane
-    constexpr float PS = 16384.0f;                         // small weights stay in fp16's normal range
+    // Weights are below 2 * 2^PS units.  The second part of a weight is taken 2^LS
+    // times as large, so that both stay in fp16's normal range down to 2^-28 of that.
+    constexpr uint32_t PS = 14;
+    constexpr float LS = 2048.0f;
     __shared__ __align__(16) float mrg[QA_NWV][16][D + 2];
     __shared__ int last;
     auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
@@ -235,18 +240,17 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             for (int i = 0; i < 8; ++i) qb[e][i] = (_Float16)(x[e][i] * down);
     }
     float m_run = -INFINITY, l_run = 0.0f;                 // head l16 % 8; the sum over this lane's tokens only
-    float ref = 0.0f;                                      // a power of two above every value scale so far; the unit of acc
+    float top = 0x1p-100f;                                 // the largest product of weight and value scale so far, of head
+                                                           // l16 % 8; acc is in units of the power of two below it, / 2^PS
+    auto expo = [](float x) { return max(__float_as_uint(x) >> 23, PS + 1u); };
+    auto unit = [&](float x) { return __uint_as_float((expo(x) - PS) << 23); };                // of acc
+    auto per_unit = [&](float x) { return __uint_as_float((254u + PS - expo(x)) << 23); };     // its reciprocal
     df4 acc[8];                                            // [channel tile][row 4 q4 + r]
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) acc[ct] = df4{0.0f, 0.0f, 0.0f, 0.0f};
-    // the softmax's step over logits z, to weights in units that make acc's
+    // the softmax's step over logits z, to products of weight and value scale;
+    // returns what takes them to acc's units
     auto weigh = [&](float (&z)[NT][4], float vs) {
-        float grow = 1.0f;                                 // of acc's unit
-        if (vs > ref) {
-            const float up = __uint_as_float((__float_as_uint(vs) & 0x7f800000u) + 0x00800000u);
-            grow = ref / up;
-            ref = up;
-        }
         float cm = -INFINITY;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -257,30 +261,33 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         const float mb = mn == -INFINITY ? 0.0f : mn;
         const float alpha = __builtin_amdgcn_exp2f(m_run - mb);
         float ls = 0.0f;
-        const float wf = ref > 0.0f ? vs * (PS / ref) : vs;    // (no scale above zero yet: vs is not finite, and stays so)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float e = __builtin_amdgcn_exp2f(z[n][r] - mb);
                 ls += e;
-                z[n][r] = e * wf;
+                z[n][r] = e * vs;
             }
         l_run = fmaf(l_run, alpha, ls);
         m_run = mn;
-        if (grow != 1.0f || !__all(alpha == 1.0f)) {       // the unit or some head's running maximum moved
+        const float was = unit(top);
+        top = fmaxf(top * alpha, __builtin_amdgcn_exp2f(cm - mb) * vs);
+        const float per = per_unit(top), grow = alpha * was * per;
+        if (!__all(grow == 1.0f)) {                        // some head's running maximum or unit moved
             float f[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {                  // alpha of head (4 q4 + r) % 8
-                const float a0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), r));
-                const float a1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), 4 + r));
-                f[r] = ((q4 & 1) ? a1 : a0) * grow;
+            for (int r = 0; r < 4; ++r) {                  // grow of head (4 q4 + r) % 8
+                const float a0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(grow), r));
+                const float a1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(grow), 4 + r));
+                f[r] = (q4 & 1) ? a1 : a0;
             }
 #pragma unroll
             for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[ct][r] *= f[r];
         }
+        return per;
     };
     auto consume = [&](const QStage<FMT, B> &st) {
         float z[NT][4];
@@ -296,15 +303,14 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[n][r] = a[r] * f;          // token TPQ q4 + 4 n + r, head l16 % 8
         }
-        weigh(z, st.vs);
+        const float per = weigh(z, st.vs), more = l16 < 8 ? 1.0f : LS, less = l16 < 8 ? 0.0f : -LS;
 #pragma unroll
         for (int s = 0; s < B / 32; ++s) {
             dhf8 pa;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w = z[2 * s + (i >> 2)][i & 3];
-                const _Float16 hi = (_Float16)w;
-                pa[i] = l16 < 8 ? hi : (_Float16)(w - (float)hi);
+            for (int i = 0; i < 8; ++i) {                  // the first part, or what it leaves
+                const float w = z[2 * s + (i >> 2)][i & 3] * per;
+                pa[i] = (_Float16)fmaf((float)(_Float16)w, less, w * more);
             }
 #pragma unroll
             for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, codes_f16<FMT>(st.v[ct][2 * s], st.v[ct][2 * s + 1]), acc[ct]);
@@ -348,18 +354,18 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             for (int r = 0; r < 4; ++r)                    // (rows behind the last token may hold anything)
                 z[n][r] = TPQ * q4 + 4 * n + r < rest ? a[r] * (scale * 1.44269504088896340736f) : -INFINITY;
         }
-        weigh(z, 1.0f);
+        const float per = weigh(z, 1.0f);
 #pragma unroll
         for (int s = 0; s < B / 32; ++s) {
             M8 pa, pl2{};                                  // bf16: a third part, its rows the first eight
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float w = z[2 * s + (i >> 2)][i & 3];
+                const float w = z[2 * s + (i >> 2)][i & 3] * per;
                 const E hi = (E)w;
                 const float r1 = w - (float)hi;
-                const E mid = (E)r1;
+                const E mid = (E)(r1 * LS);
                 pa[i] = l16 < 8 ? hi : mid;
-                if (DT) pl2[i] = l16 < 8 ? (E)(r1 - (float)mid) : (E)0.0f;
+                if (DT) pl2[i] = l16 < 8 ? (E)(r1 - (float)mid * (1.0f / LS)) : (E)0.0f;
             }
             const int keep = rest - (TPQ * q4 + 8 * s);    // tokens of the lane's eight
 #pragma unroll
@@ -377,16 +383,18 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     }
     // join the waves
     l_run = rows_all(l_run, [](float a, float b) { return a + b; });
-    const float back = ref * (1.0f / PS);
     int lane = tid;
     asm volatile("" : "+v"(lane));
     lane &= 63;
     const int row = lane >> 4, col = lane & 15;   // (worked out again, as above)
-    if (lane < 16) { mrg[wave][col][0] = m_run; mrg[wave][col][1] = l_run; }
+    if (lane < 16) {                                       // a head's unit stands in the row of its second parts
+        mrg[wave][col][0] = lane < 8 ? m_run : unit(top);
+        mrg[wave][col][1] = l_run;
+    }
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) mrg[wave][4 * row + r][2 + 16 * ct + col] = acc[ct][r] * back;
+        for (int r = 0; r < 4; ++r) mrg[wave][4 * row + r][2 + 16 * ct + col] = acc[ct][r];
     __syncthreads();
     float *out = outp + (uint64_t)p * q.G * D;
     // partials of a pair's runs are consecutive: run 0's is this workgroup's less pl.i
@@ -402,8 +410,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         for (int w = 0; w < QA_NWV; ++w) {
             const float f = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[w] - M);
             const float2 u = *(const float2 *)&mrg[w][h][2 + c], v = *(const float2 *)&mrg[w][h + 8][2 + c];
-            A.x += (u.x + v.x) * f;
-            A.y += (u.y + v.y) * f;
+            const float fu = f * mrg[w][h + 8][0];
+            A.x += fmaf(v.x, 1.0f / LS, u.x) * fu;
+            A.y += fmaf(v.y, 1.0f / LS, u.y) * fu;
             S += mrg[w][h][1] * f;
         }
         if (pl.ns == 1) {

@@ -1,9 +1,14 @@
-"""Attention over the 8-bit cache for every value that the types hold."""
+"""Attention over the 8-bit cache for every value that the types hold: value
+scales far apart, with the softmax's weight on any of them, and values that are
+not finite, wherever they stand.  Against tests/_quant.py, within the error
+that the arithmetic allows (_quant.bound)."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
+import _quant as R
 import paper_2607_00760_amd as M
 
 pytestmark = pytest.mark.gpu
@@ -21,6 +26,84 @@ def make(fmt, dtype, block, S, H, G, cap):
         if n != "lens":
             getattr(c, n).view(torch.uint8).fill_(0xff)
     return c
+
+
+def check(c, k, v, q, G, where):
+    """k, v [H][n][D], q [H * G][D] of one sequence: every head for itself."""
+    c.append(k[None].cuda(), v[None].cuda())
+    out, part = c.decode(q[None].cuda(), SCALE)[0], c.decode_selected(q[None].cuda(), SCALE, (2, 3))[0]
+    p = c.params
+    for h in range(k.shape[0]):
+        r = R.Pair(k[h], v[h], p.format, p.block)
+        at = slice(h * G, (h + 1) * G)
+        for got, picked, name in ((out, None, "all"), (part, r.select(q[at].float().numpy(), 2, 3), "selected")):
+            for g in range(G):
+                qs = q[h * G + g][None].float().numpy()
+                want, zmax = r.attend(qs, SCALE, picked)
+                x = got[h * G + g].double().cpu().numpy()
+                assert np.isfinite(x).all(), f"{where} {name} head {g}"
+                rel = np.linalg.norm(x - want[0]) / np.linalg.norm(want)
+                assert rel < R.bound(zmax), f"{where} {name} head {g}: rel {rel:.2e} of {R.bound(zmax):.2e}"
+
+
+def apart(fmt, dtype, block, bits, nb, tail, big):
+    """Blocks of values about 2^`bits` apart; big(b): whether block b (nb: the
+    unfinished one) is a large one.  Keys of large blocks lie against a sign
+    vector, the others along it: the heads put their weight on the small blocks,
+    on the large ones, on both alike, and where the two products are alike."""
+    B, G, dt = block, 4, DT[dtype]
+    g = torch.Generator().manual_seed(bits + nb)
+    n = nb * B + tail
+    u = torch.sign(torch.randn(D, generator=g))
+    is_big = torch.tensor([big(i // B) for i in range(n)])
+    top = min(13, bits // 2) if dtype == "fp16" else bits // 2
+    v = torch.randn(n, D, generator=g)
+    v = (v * torch.where(is_big, 2.0 ** top, 2.0 ** (top - bits))[:, None]).to(dt)
+    k = (u * torch.where(is_big, -1.0, 1.0)[:, None] + 0.05 * torch.randn(n, D, generator=g)).to(dt)
+    # z = +-SCALE * D * a; the large blocks' weight is exp(-2 z)
+    unit = math.log(2.0) / (2 * SCALE * D)
+    a = torch.tensor([min(bits + 30.0, 120.0) * unit, -20.0 * unit, 0.0, min(bits, 60.0) * unit])
+    q = (a[:, None] * u + 0.02 * torch.randn(G, D, generator=g)).to(dt)
+    check(make(fmt, dtype, B, 1, 1, G, n), k[None], v[None], q, G, f"{bits} bits, {nb} blocks + {tail}")
+
+
+@pytest.mark.parametrize("fmt,dtype,block", FORMS)
+def test_value_scales_apart(fmt, dtype, block):
+    """A wave meets large blocks before small ones and the other way round; runs
+    of large blocks are joined with runs of small ones."""
+    for bits in (20, 28, 30) if dtype == "fp16" else (24, 32, 40, 90, 200):
+        for nb, big in ((9, lambda b: b < 4), (9, lambda b: b >= 5), (40, lambda b: b % 8 < 4), (70, lambda b: b < 40)):
+            apart(fmt, dtype, block, bits, nb, 0, big)
+
+
+@pytest.mark.parametrize("fmt,dtype,block", FORMS)
+def test_unfinished_block_apart(fmt, dtype, block):
+    """The unfinished block's values far above or below the whole blocks', or alone."""
+    for bits in (20, 30) if dtype == "fp16" else (40, 100, 200):
+        for nb in (0, 1, 8, 40):
+            apart(fmt, dtype, block, bits, nb, 7, lambda b: b == nb)
+            apart(fmt, dtype, block, bits, nb, block - 1, lambda b: b < nb)
+
+
+@pytest.mark.parametrize("fmt,dtype,block", FORMS)
+def test_unfinished_block_of_mixed_values(fmt, dtype, block):
+    """Tokens of the unfinished block of very different magnitudes, the weight
+    on the small ones, on the large ones, or where the products are alike."""
+    dt, G = DT[dtype], 3
+    g = torch.Generator().manual_seed(23)
+    bits = 20 if dtype == "fp16" else 100
+    top = 14 if dtype == "fp16" else 50
+    for n in (block - 1, 2 * block + 9):
+        u = torch.sign(torch.randn(D, generator=g))
+        large = torch.arange(n) % 3 == 0
+        v = (torch.randn(n, D, generator=g) * torch.where(large, 2.0 ** (top - 2), 2.0 ** (top - bits))[:, None]).to(dt)
+        if n > block:
+            v[: n // block * block] = torch.randn(n // block * block, D, generator=g).to(dt)
+        k = (u * torch.where(large, -1.0, 1.0)[:, None] + 0.05 * torch.randn(n, D, generator=g)).to(dt)
+        unit = math.log(2.0) / (2 * SCALE * D)
+        a = torch.tensor([min(bits + 30.0, 120.0) * unit, -20.0 * unit, min(bits, 60.0) * unit])
+        q = (a[:, None] * u + 0.02 * torch.randn(G, D, generator=g)).to(dt)
+        check(make(fmt, dtype, block, 1, 1, G, n), k[None], v[None], q, G, f"{n} tokens")
 
 
 @pytest.mark.parametrize("fmt,dtype,block", FORMS)
