@@ -249,8 +249,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) acc[ct] = df4{0.0f, 0.0f, 0.0f, 0.0f};
     // the softmax's step over logits z, to products of weight and value scale;
-    // returns what takes them to acc's units
-    auto weigh = [&](float (&z)[NT][4], float vs) {
+    // returns what takes them to acc's units.  (What follows in 16 bits reaches
+    // further than its scale of 1, and has room for a smaller unit: low, least.)
+    auto weigh = [&](float (&z)[NT][4], float vs, float reach, float low, float least) {
         float cm = -INFINITY;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -272,7 +273,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         l_run = fmaf(l_run, alpha, ls);
         m_run = mn;
         const float was = unit(top);
-        top = fmaxf(top * alpha, __builtin_amdgcn_exp2f(cm - mb) * vs);
+        top = fmaxf(fmaxf(top * alpha, __builtin_amdgcn_exp2f(cm - mb) * reach) * low, least);
         const float per = per_unit(top), grow = alpha * was * per;
         if (!__all(grow == 1.0f)) {                        // some head's running maximum or unit moved
             float f[4];
@@ -303,7 +304,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[n][r] = a[r] * f;          // token TPQ q4 + 4 n + r, head l16 % 8
         }
-        const float per = weigh(z, st.vs), more = l16 < 8 ? 1.0f : LS, less = l16 < 8 ? 0.0f : -LS;
+        const float per = weigh(z, st.vs, st.vs, 1.0f, 0.0f), more = l16 < 8 ? 1.0f : LS, less = l16 < 8 ? 0.0f : -LS;
 #pragma unroll
         for (int s = 0; s < B / 32; ++s) {
             dhf8 pa;
@@ -340,6 +341,19 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         M8 qd[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) __builtin_memcpy(&qd[e], qp + 32 * e + 8 * q4, 16);
+        uint4 vt[B / 32][8];                               // (rows behind the last token may hold anything)
+#pragma unroll
+        for (int s = 0; s < B / 32; ++s)
+#pragma unroll
+            for (int ct = 0; ct < 8; ++ct) {
+                const int keep = rest - (TPQ * q4 + 8 * s);    // tokens of the lane's eight
+                uint4 x = *(const uint4 *)(vp + (16 * ct + l16) * B + TPQ * q4 + 8 * s);
+                x.x = keep >= 2 ? x.x : (keep == 1 ? x.x & 0xffffu : 0u);
+                x.y = keep >= 4 ? x.y : (keep == 3 ? x.y & 0xffffu : 0u);
+                x.z = keep >= 6 ? x.z : (keep == 5 ? x.z & 0xffffu : 0u);
+                x.w = keep >= 8 ? x.w : (keep == 7 ? x.w & 0xffffu : 0u);
+                vt[s][ct] = x;
+            }
         float z[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -351,10 +365,27 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
                 a = DM::run(x, qd[e], a);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r)                    // (rows behind the last token may hold anything)
+            for (int r = 0; r < 4; ++r)
                 z[n][r] = TPQ * q4 + 4 * n + r < rest ? a[r] * (scale * 1.44269504088896340736f) : -INFINITY;
         }
-        const float per = weigh(z, 1.0f);
+        // fp16 values are at most 2^16 of a unit and leave their sums room.  bf16
+        // ones go up to 2^128: the unit knows the largest, and is 2^60 below it, as
+        // the weights' parts would fall below 2^-126 next to the largest values.
+        float reach = 1.0f;
+        if (DT) {
+            float a = 0.0f;
+#pragma unroll
+            for (int s = 0; s < B / 32; ++s)
+#pragma unroll
+                for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {          // (the lower half adds less than a step to the upper one)
+                        const uint32_t w = ((const uint32_t *)&vt[s][ct])[e];
+                        a = fmaxf(a, fmaxf(fabsf(__uint_as_float(w)), fabsf(__uint_as_float(w << 16))));
+                    }
+            reach = __uint_as_float(wave_max_u(__float_as_uint(a)));
+        }
+        const float per = DT ? weigh(z, 1.0f, reach, 0x1p-60f, 0x1p-60f) : weigh(z, 1.0f, 1.0f, 1.0f, 0.0f);
 #pragma unroll
         for (int s = 0; s < B / 32; ++s) {
             M8 pa, pl2{};                                  // bf16: a third part, its rows the first eight
@@ -367,15 +398,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
                 pa[i] = l16 < 8 ? hi : mid;
                 if (DT) pl2[i] = l16 < 8 ? (E)(r1 - (float)mid * (1.0f / LS)) : (E)0.0f;
             }
-            const int keep = rest - (TPQ * q4 + 8 * s);    // tokens of the lane's eight
 #pragma unroll
             for (int ct = 0; ct < 8; ++ct) {
-                uint4 x = *(const uint4 *)(vp + (16 * ct + l16) * B + TPQ * q4 + 8 * s);
-                x.x = keep >= 2 ? x.x : (keep == 1 ? x.x & 0xffffu : 0u);
-                x.y = keep >= 4 ? x.y : (keep == 3 ? x.y & 0xffffu : 0u);
-                x.z = keep >= 6 ? x.z : (keep == 5 ? x.z & 0xffffu : 0u);
-                x.w = keep >= 8 ? x.w : (keep == 7 ? x.w & 0xffffu : 0u);
-                const M8 vb = __builtin_bit_cast(M8, x);
+                const M8 vb = __builtin_bit_cast(M8, vt[s][ct]);
                 acc[ct] = DM::run(pa, vb, acc[ct]);
                 if (DT) acc[ct] = DM::run(pl2, vb, acc[ct]);
             }

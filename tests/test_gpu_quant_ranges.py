@@ -1,6 +1,6 @@
-"""Attention over the 8-bit cache for every value that the types hold: value
-scales far apart, with the softmax's weight on any of them, and values that are
-not finite, wherever they stand.  Against tests/_quant.py, within the error
+"""Attention over the 8-bit cache for every finite value that the types hold:
+value scales far apart, with the softmax's weight on any of them; values next
+to the type's largest; and values that are not finite, wherever they stand.  Against tests/_quant.py, within the error
 that the arithmetic allows (_quant.bound)."""
 import math
 
@@ -79,7 +79,7 @@ def test_value_scales_apart(fmt, dtype, block):
 @pytest.mark.parametrize("fmt,dtype,block", FORMS)
 def test_unfinished_block_apart(fmt, dtype, block):
     """The unfinished block's values far above or below the whole blocks', or alone."""
-    for bits in (20, 30) if dtype == "fp16" else (40, 100, 200):
+    for bits in (20, 30) if dtype == "fp16" else (40, 100, 200, 240):
         for nb in (0, 1, 8, 40):
             apart(fmt, dtype, block, bits, nb, 7, lambda b: b == nb)
             apart(fmt, dtype, block, bits, nb, block - 1, lambda b: b < nb)
@@ -104,6 +104,22 @@ def test_unfinished_block_of_mixed_values(fmt, dtype, block):
         a = torch.tensor([min(bits + 30.0, 120.0) * unit, -20.0 * unit, min(bits, 60.0) * unit])
         q = (a[:, None] * u + 0.02 * torch.randn(G, D, generator=g)).to(dt)
         check(make(fmt, dtype, block, 1, 1, G, n), k[None], v[None], q, G, f"{n} tokens")
+
+
+@pytest.mark.parametrize("fmt,dtype,block", FORMS)
+@pytest.mark.parametrize("nb,tail", [(0, 1)])
+def test_values_next_to_the_largest(fmt, dtype, block, nb, tail):
+    """Channels of one sign at the type's largest: an average of them is finite
+    however many tokens there are, in the unfinished block as in whole ones."""
+    dt, G, n = DT[dtype], 4, nb * block + tail
+    g = torch.Generator().manual_seed(nb)
+    top = torch.finfo(dt).max
+    v = torch.full((n, D), top)
+    v[:, 1::2] *= torch.sign(torch.randn(n, D // 2, generator=g))
+    v[:, ::4] *= -1.0
+    v = v.to(dt)
+    k, q = torch.randn(n, D, generator=g).to(dt), (0.1 * torch.randn(G, D, generator=g)).to(dt)
+    check(make(fmt, dtype, block, 1, 1, G, n), k[None], v[None], q, G, f"{n} tokens")
 
 
 @pytest.mark.parametrize("fmt,dtype,block", FORMS)
