@@ -44,7 +44,7 @@ constexpr int QA_LEAST = 2 * QA_NWV, QA_FEW = 256;
 // 4 heads): 1 x 4117 tokens 9.7 -> 9.3.
 constexpr int QA_ALONE = 16, QA_JOIN = 16;
 constexpr int QA_HEADS = 8;
-constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and accumulators of the heads
+constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and averages of the heads
 
 // 8 codes as fp16
 template <int FMT> __device__ __forceinline__ dhf8 codes_f16(uint32_t a, uint32_t b) {
@@ -74,7 +74,9 @@ template <int FMT, int B> struct QStage {                  // a block in flight
     float ks, vs;
 };
 
-__device__ __forceinline__ float joined(float a, float s) { return s > 0.0f ? a / s : (s != s ? s : 0.0f); }
+// what weights that sum to s are multiplied by in an average.  (Averages are
+// joined, not sums: a sum of values next to the type's largest overflows.)
+__device__ __forceinline__ float share_of(float s) { return s > 0.0f ? 1.0f / s : (s != s ? s : 0.0f); }
 
 // partials, past the XCD's L2
 __device__ __forceinline__ void put2(float *p, float2 x) {
@@ -110,19 +112,26 @@ __device__ __forceinline__ Joined join_runs(const float *part, int stride, int n
                 if (r0 + e * np >= ns) ml[e] = make_float2(-INFINITY, 0.0f);
                 mn = fmaxf(mn, ml[e].x);
             }
-            const float mb = mn == -INFINITY ? 0.0f : mn, x = __builtin_amdgcn_exp2f(M - mb);
-            A = make_float4(A.x * x, A.y * x, A.z * x, A.w * x);
-            S *= x;
+            const float mb = mn == -INFINITY ? 0.0f : mn;
+            S *= __builtin_amdgcn_exp2f(M - mb);
             M = mn;
+            float s = S;
+#pragma unroll
+            for (int e = 0; e < CB; ++e) {
+                ml[e].y *= __builtin_amdgcn_exp2f(ml[e].x - mb);
+                s += ml[e].y;
+            }
+            const float inv = share_of(s), x = S * inv;
+            A = make_float4(A.x * x, A.y * x, A.z * x, A.w * x);
+            S = s;
 #pragma unroll
             for (int e = 0; e < CB; ++e) {
                 if (r0 + e * np >= ns) continue;
-                const float y = __builtin_amdgcn_exp2f(ml[e].x - mb);
+                const float y = ml[e].y * inv;
                 A.x = fmaf(a[e][0].x, y, A.x);
                 A.y = fmaf(a[e][0].y, y, A.y);
                 A.z = fmaf(a[e][1].x, y, A.z);
                 A.w = fmaf(a[e][1].y, y, A.w);
-                S = fmaf(ml[e].y, y, S);
             }
         }
     float *x = lds + 8 * tid;
@@ -137,9 +146,12 @@ __device__ __forceinline__ Joined join_runs(const float *part, int stride, int n
             const float *o = lds + 8 * (tid + e * cols);
             const float4 a = *(const float4 *)o;
             const float mn = fmaxf(M, o[4]), mb = mn == -INFINITY ? 0.0f : mn;
-            const float x = __builtin_amdgcn_exp2f(M - mb), y = __builtin_amdgcn_exp2f(o[4] - mb);
+            float x = S * __builtin_amdgcn_exp2f(M - mb), y = o[5] * __builtin_amdgcn_exp2f(o[4] - mb);
+            S = x + y;
+            const float inv = share_of(S);
+            x *= inv;
+            y *= inv;
             A = make_float4(A.x * x + a.x * y, A.y * x + a.y * y, A.z * x + a.z * y, A.w * x + a.w * y);
-            S = S * x + o[5] * y;
             M = mn;
         }
     return Joined{M, S, A};
@@ -430,18 +442,22 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
 #pragma unroll
         for (int w = 0; w < QA_NWV; ++w) { m[w] = mrg[w][h][0]; M = fmaxf(M, m[w]); }
         float2 A = make_float2(0.0f, 0.0f);
-        float S = 0.0f;
+        float f[QA_NWV], S = 0.0f;
 #pragma unroll
         for (int w = 0; w < QA_NWV; ++w) {
-            const float f = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[w] - M);
+            f[w] = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[w] - M);
+            S += mrg[w][h][1] * f[w];
+        }
+        const float inv = share_of(S);
+#pragma unroll
+        for (int w = 0; w < QA_NWV; ++w) {
             const float2 u = *(const float2 *)&mrg[w][h][2 + c], v = *(const float2 *)&mrg[w][h + 8][2 + c];
-            const float fu = f * mrg[w][h + 8][0];
+            const float fu = f[w] * inv * mrg[w][h + 8][0];
             A.x += fmaf(v.x, 1.0f / LS, u.x) * fu;
             A.y += fmaf(v.y, 1.0f / LS, u.y) * fu;
-            S += mrg[w][h][1] * f;
         }
         if (pl.ns == 1) {
-            *(float2 *)(out + i) = make_float2(joined(A.x, S), joined(A.y, S));
+            *(float2 *)(out + i) = A;
         } else {
             put2(mine + 2 * QA_HEADS + i, A);
             if (c == 0) put2(mine + 2 * h, make_float2(M, S));
@@ -468,7 +484,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     }
     if (!last_of(arrivals + p, ns, last)) return;
     const Joined j = join_runs(first, stride, ns, q.G, &mrg[0][0][0]);
-    if (tid < 32 * q.G) *(float4 *)(out + 4 * tid) = make_float4(joined(j.A.x, j.S), joined(j.A.y, j.S), joined(j.A.z, j.S), joined(j.A.w, j.S));
+    if (tid < 32 * q.G) *(float4 *)(out + 4 * tid) = j.A;
 }
 
 }  // namespace

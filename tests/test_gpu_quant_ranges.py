@@ -107,7 +107,7 @@ def test_unfinished_block_of_mixed_values(fmt, dtype, block):
 
 
 @pytest.mark.parametrize("fmt,dtype,block", FORMS)
-@pytest.mark.parametrize("nb,tail", [(0, 1)])
+@pytest.mark.parametrize("nb,tail", [(0, 1), (0, 5), (1, 0), (9, 31), (70, 3), (700, 1)])
 def test_values_next_to_the_largest(fmt, dtype, block, nb, tail):
     """Channels of one sign at the type's largest: an average of them is finite
     however many tokens there are, in the unfinished block as in whole ones."""
