@@ -5,10 +5,10 @@
 // out = sum_t p_t v_t / sum_t p_t, p_t = exp(scale q.k_t - max), with k_t and
 // v_t their codes times their block's scale.  One pass with running maximum
 // and sum: a wave takes a block at a time, straight from memory into matrix
-// operands.  Both products are fp16: a code of either format is an fp16 value,
-// a query of 8 or 11 bits too (bf16 after a power of two per head), and the
-// weights take part as two fp16 parts, 22 bits, in rows 0..7 and 8..15 of the
-// left operand, which groups of up to 8 heads leave room for.  A block's value
+// operands.  A code of either format is a value of both 16-bit types, so the
+// logits' product is of the query's type and exact.  The outputs' product is
+// fp16: the weights take part as two fp16 parts, 22 bits, in rows 0..7 and 8..15
+// of the left operand, which groups of up to 8 heads leave room for.  A block's value
 // scale goes into its weights; the unit of a head's sums is a power of two that
 // follows the largest product of weight and scale, so that a block is as exact
 // as its share of the output asks, however far apart the scales are.
@@ -66,6 +66,31 @@ template <int FMT> __device__ __forceinline__ dhf8 codes_f16(uint32_t a, uint32_
     dhf8 r;
     __builtin_memcpy(&r, o, 16);
     return r;
+}
+
+// 8 codes as bf16: of the format's conversion, or the upper halves of fp32 integers
+template <int FMT> __device__ __forceinline__ DMma<1>::v8 codes_bf16(uint32_t a, uint32_t b) {
+    uint32_t o[4];
+    const uint32_t w[2] = {a, b};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (FMT == QF_E4M3) {
+            o[2 * i] = e4m3x2<1, false>(w[i]);
+            o[2 * i + 1] = e4m3x2<1, true>(w[i]);
+        } else {
+            const uint32_t x0 = __float_as_uint((float)(int8_t)w[i]), x1 = __float_as_uint((float)(int8_t)(w[i] >> 8));
+            const uint32_t x2 = __float_as_uint((float)(int8_t)(w[i] >> 16)), x3 = __float_as_uint((float)(int8_t)(w[i] >> 24));
+            o[2 * i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+            o[2 * i + 1] = __builtin_amdgcn_perm(x3, x2, 0x07060302u);
+        }
+    }
+    DMma<1>::v8 r;
+    __builtin_memcpy(&r, o, 16);
+    return r;
+}
+template <int FMT, int DT> __device__ __forceinline__ typename DMma<DT>::v8 codes_of(uint32_t a, uint32_t b) {
+    if constexpr (DT) return codes_bf16<FMT>(a, b);
+    else return codes_f16<FMT>(a, b);
 }
 
 template <int FMT, int B> struct QStage {                  // a block in flight
@@ -224,8 +249,8 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     int id0 = 0, id1 = 0;
     if (t < b1) { id0 = block_at(t); id1 = block_at(t + QA_NWV); }
     // q operand: column l16 is head l16 % 8, inner index (j, half, q4, i) channel 64 j + 16 q4 + 8 half + i
-    dhf8 qb[4];
-    float zs;                                              // softmax scale in powers of two, and q's
+    typename DM::v8 qb[4];
+    float zs = scale * 1.44269504088896340736f;            // softmax scale in powers of two, and q's
     {
         uint16_t w[4][8];
 #pragma unroll
@@ -233,23 +258,24 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         __builtin_amdgcn_sched_barrier(0);
         if (t < b1) load(id0, st0);                        // on its way while q is looked at
         __builtin_amdgcn_sched_barrier(0);
-        float x[4][8], a = 0.0f;
+        if (DT) {                                          // largest magnitude in [1, 2): products with codes stay in range
+            float x[4][8], a = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { x[e][i] = h2f(w[e][i], DT); a = fmaxf(a, fabsf(x[e][i])); }
-        float down = 1.0f;
-        zs = scale * 1.44269504088896340736f;
-        if (DT) {                                          // largest magnitude in [1, 2), what falls below 2^-24 of it is lost
+                for (int i = 0; i < 8; ++i) { x[e][i] = h2f(w[e][i], DT); a = fmaxf(a, fabsf(x[e][i])); }
             a = rows_all(a, [](float m, float o) { return fmaxf(m, o); });
             const uint32_t e = min(max(__float_as_uint(a) >> 23, 1u), 253u);
-            down = __uint_as_float((254u - e) << 23);
+            const float down = __uint_as_float((254u - e) << 23);
             zs *= __uint_as_float(e << 23);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) qb[e][i] = (typename DM::el)(x[e][i] * down);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) __builtin_memcpy(&qb[e], w[e], 16);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) qb[e][i] = (_Float16)(x[e][i] * down);
     }
     float m_run = -INFINITY, l_run = 0.0f;                 // head l16 % 8; the sum over this lane's tokens only
     float top = 0x1p-100f;                                 // the largest product of weight and value scale so far, of head
@@ -309,8 +335,8 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             df4 a = df4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                a = DMma<0>::run(codes_f16<FMT>(st.k[n][j].x, st.k[n][j].y), qb[2 * j], a);
-                a = DMma<0>::run(codes_f16<FMT>(st.k[n][j].z, st.k[n][j].w), qb[2 * j + 1], a);
+                a = DM::run(codes_of<FMT, DT>(st.k[n][j].x, st.k[n][j].y), qb[2 * j], a);
+                a = DM::run(codes_of<FMT, DT>(st.k[n][j].z, st.k[n][j].w), qb[2 * j + 1], a);
             }
             const float f = zs * st.ks;
 #pragma unroll

@@ -1,6 +1,7 @@
 """Attention over the 8-bit cache for every finite value that the types hold:
 value scales far apart, with the softmax's weight on any of them; values next
-to the type's largest; and values that are not finite, wherever they stand.  Against tests/_quant.py, within the error
+to the type's largest; queries of very different channels; and values that are
+not finite, wherever they stand.  Against tests/_quant.py, within the error
 that the arithmetic allows (_quant.bound)."""
 import math
 
@@ -120,6 +121,22 @@ def test_values_next_to_the_largest(fmt, dtype, block, nb, tail):
     v = v.to(dt)
     k, q = torch.randn(n, D, generator=g).to(dt), (0.1 * torch.randn(G, D, generator=g)).to(dt)
     check(make(fmt, dtype, block, 1, 1, G, n), k[None], v[None], q, G, f"{n} tokens")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("block", [32, 64])
+@pytest.mark.parametrize("bits", [18, 24, 30, 60, 100])
+def test_queries_of_far_channels(fmt, block, bits):
+    """A bf16 query whose largest channel meets keys of zero: the others, 2^`bits`
+    below it, make the logits."""
+    G, n = 3, 9 * block + 5
+    g = torch.Generator().manual_seed(bits)
+    k, v = torch.randn(n, D, generator=g), torch.randn(n, D, generator=g)
+    k[:, 7] = 0.0
+    q = torch.randn(G, D, generator=g)
+    q[:, 7] = 2.0 ** bits
+    q[1] *= 2.0 ** -3
+    check(make(fmt, "bf16", block, 1, 1, G, n), k.bfloat16()[None], v.bfloat16()[None], q.bfloat16(), G, f"{bits} bits")
 
 
 @pytest.mark.parametrize("fmt,dtype,block", FORMS)
