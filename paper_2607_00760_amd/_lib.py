@@ -86,12 +86,18 @@ def load() -> C.CDLL:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: build it with paper_2607_00760_amd.build.build() "
                               "(there is no fallback path)")
-        _lib = bind_signatures(C.CDLL(LIB_PATH))
+        lib = C.CDLL(LIB_PATH)
+        missing = [n for n in EXPORTED if not hasattr(lib, n)]
+        if missing:
+            raise ImportError(f"{LIB_PATH} lacks {', '.join(missing)}: it is older than this package, build it again with "
+                              "paper_2607_00760_amd.build.build()")
+        _lib = bind_signatures(lib)
     return _lib
 
 
 def bind_signatures(L: C.CDLL) -> C.CDLL:
-    """Set the argument and result types of every exported entry point of L."""
+    """Set the argument and result types of the exported entry points of L (one
+    that holds the cache's host layer alone lacks some of them)."""
     vp, sz = C.c_void_p, C.c_size_t
     L.mosaic_params_default.argtypes = [C.POINTER(MosaicParams)]
     L.mosaic_params_default.restype = None
@@ -128,7 +134,7 @@ def bind_signatures(L: C.CDLL) -> C.CDLL:
     L.mosaic_seq_tokens.restype = C.c_int32
     L.mosaic_last_error.argtypes = []
     L.mosaic_last_error.restype = C.c_char_p
-    if hasattr(L, "mosaic_quant_append"):                   # (a library of the cache's host layer alone has the rest)
+    if hasattr(L, "mosaic_quant_append"):
         qc = C.POINTER(MosaicQuantCache)                   # (rows and strides also come as packed bytes)
         L.mosaic_qk_norm_rope.argtypes = [vp, vp, vp] + [C.c_int32] * 6 + [vp, vp, C.c_float, vp, C.c_int32, vp, vp, C.c_int32, C.c_int32,
                                                                          vp]
