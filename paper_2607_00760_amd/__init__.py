@@ -570,10 +570,12 @@ class QuantCache:
             self.lens.zero_()
             return
         if not isinstance(seqs, torch.Tensor):
-            seqs = [int(s) for s in seqs]
-            if any(not 0 <= s < self.num_seqs for s in seqs):
+            seqs = sorted({int(s) for s in seqs})
+            if seqs and not 0 <= seqs[0] <= seqs[-1] < self.num_seqs:
                 raise ValueError(f"sequences {seqs} of {self.num_seqs}")
-            seqs = torch.tensor(seqs, dtype=torch.int32, device=self.device)
+            for s in seqs:                                     # (nothing is copied: a graph can record it)
+                self.lens[s].zero_()
+            return
         if seqs.dtype not in (torch.int32, torch.int64) or seqs.device != self.device or seqs.dim() != 1:
             raise ValueError("seqs must be a list of indices or a one-dimensional integer tensor on the cache's GPU")
         named = (torch.arange(self.num_seqs, device=self.device)[:, None] == seqs).any(1)

@@ -1,0 +1,37 @@
+"""Calls around the 8-bit cache and the norm-and-rotation pass that a program
+may make beside the ordinary ones."""
+import pytest
+import torch
+
+import paper_2607_00760_amd as M
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+
+
+def test_reset_of_a_list_is_captured():
+    """Emptying named sequences copies nothing to the device: a graph records
+    it, with the appends that follow, and every replay empties them again."""
+    S, H, B = 5, 2, 32
+    c = M.QuantCache(M.QuantParams(H, 4, "bf16", "e4m3", B), S, 4 * B)
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(S, H, 37, D, generator=g).bfloat16().cuda()
+    c.append(x, x)
+    c.reset([])
+    assert c.lens.tolist() == [[37] * H] * S
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.reset([3, 1, 3])
+        c.append(x[:, :, :2], x[:, :, :2])
+    torch.cuda.current_stream().wait_stream(side)
+    assert c.lens.tolist() == [[n] * H for n in (39, 2, 39, 2, 39)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.reset([3, 1, 3])
+        c.append(x[:, :, :2], x[:, :, :2])
+    for i in range(1, 4):
+        graph.replay()
+        assert c.lens.tolist() == [[n] * H for n in (39 + 2 * i, 2, 39 + 2 * i, 2, 39 + 2 * i)], i
+        assert torch.equal(c.k_tail[1, :, :2], x[1, :, :2])
