@@ -8,10 +8,12 @@
 // operands.  A code of either format is a value of both 16-bit types, so the
 // logits' product is of the query's type and exact.  The outputs' product is
 // fp16: the weights take part as two fp16 parts, 22 bits, in rows 0..7 and 8..15
-// of the left operand, which groups of up to 8 heads leave room for.  A block's value
-// scale goes into its weights; the unit of a head's sums is a power of two that
-// follows the largest product of weight and scale, so that a block is as exact
-// as its share of the output asks, however far apart the scales are.
+// of the left operand, which groups of up to 8 heads leave room for.  (A third
+// part changes no measured error, 4e-7 to 5e-7 of the outputs for 4 K tokens,
+// 7e-7 in 32 bits throughout, and takes 1 to 2 %.)  A block's value scale goes
+// into its weights; the unit of a head's sums is a power of two that follows the
+// largest product of weight and scale, so that a block is as exact as its share
+// of the output asks, however far apart the scales are.
 //
 // The products' layouts ask for 8 tokens of one channel in a lane: values lie
 // by channel in the cache, and the rows of the first product are dealt so that
