@@ -461,8 +461,9 @@ mosaic_status mosaic_dense_decode_attention(const void *q, const void *k, const 
  *   inv_freq     : fp32 [rot_dim / 2]; rot_dim is a multiple of 16 up to 128
  * Strides are host arrays.  num_seqs or num_tokens 0: OK, nothing enqueued.
  * A row with a NaN or an infinity spoils itself only.
- * Errors: INVALID (NULL, shape, alignment, strides), UNSUPPORTED (head_dim
- * != 128, rot_dim, 2^23 tokens or more). */
+ * Errors: INVALID (NULL, shape, alignment, strides, an output whose rows
+ * overlap along a dimension), UNSUPPORTED (head_dim != 128, rot_dim, 2^23
+ * tokens or more). */
 typedef struct {
     const void *in;
     void *out;

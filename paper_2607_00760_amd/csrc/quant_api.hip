@@ -94,6 +94,14 @@ hipError_t attend(const mosaic_quant_cache *c, const QCache &qc, const void *q, 
 
 bool bad_strides(const int64_t *s) { return (s[0] | s[1] | s[2]) % 8 != 0; }
 
+// rows of an output that share memory, along one of its dimensions
+bool rows_overlap(const int64_t *s, int n0, int n1, int n2) {
+    const int n[3] = {n0, n1, n2};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && s[i] > -D && s[i] < D) return true;
+    return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -175,6 +183,8 @@ mosaic_status mosaic_qk_norm_rope(const mosaic_rows *q, const mosaic_rows *k, co
         if (!r->in || !r->out) return fail(MOSAIC_ERR_INVALID, "NULL rows");
         if (off16(r->in) || off16(r->out) || bad_strides(r->in_strides) || bad_strides(r->out_strides))
             return fail(MOSAIC_ERR_INVALID, "rows must be 16-byte aligned, their strides multiples of 8 elements");
+        if (rows_overlap(r->out_strides, num_seqs, num_tokens, i == 0 ? q_heads : kv_heads))
+            return fail(MOSAIC_ERR_INVALID, "rows of an output overlap");
         (i == 0 ? a.q : (i == 1 ? a.k : a.vp)) = NormRope::Part{(const uint16_t *)r->in, (uint16_t *)r->out, r->in_strides[0], r->in_strides[1],
                                                                r->in_strides[2], r->out_strides[0], r->out_strides[1], r->out_strides[2]};
     }

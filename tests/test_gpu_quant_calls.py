@@ -35,3 +35,15 @@ def test_reset_of_a_list_is_captured():
         graph.replay()
         assert c.lens.tolist() == [[n] * H for n in (39 + 2 * i, 2, 39 + 2 * i, 2, 39 + 2 * i)], i
         assert torch.equal(c.k_tail[1, :, :2], x[1, :, :2])
+
+
+def test_outputs_whose_rows_overlap_are_refused():
+    S, n, H = 2, 3, 4
+    x = torch.randn(S, n, H, D, device="cuda").half()
+    pos, inv = torch.zeros(S, n, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda")
+    one = torch.empty(1, 1, 1, D, dtype=torch.float16, device="cuda")
+    for name, shape in (("q_out", (S, n, H, D)), ("k_out", (S, H, n, D)), ("v_out", (S, H, n, D))):
+        with pytest.raises(M.MosaicError, match="overlap"):
+            M.qk_norm_rope(x, x, pos, inv, v=x, **{name: one.expand(shape)})
+    q, k = M.qk_norm_rope(x[:1, :1, :1].expand(S, n, H, D), x, pos, inv)      # an input may repeat its rows
+    assert torch.equal(q, q[:1, :1, :1].expand_as(q))

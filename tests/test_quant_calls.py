@@ -1,0 +1,25 @@
+"""Further calls of the operators around the 8-bit cache on the CPU: what is
+refused before anything is enqueued, and what is not (over the recording HIP
+runtime of tests/test_quant_args.py)."""
+import pytest
+
+from test_quant_args import FAKE, INVALID, OK, _lib, append, cache, lib, refused, rope, three  # noqa: F401
+
+
+def rows(ins=(4096, 4096, 128), outs=(4096, 4096, 128)):
+    return _lib.MosaicRows(FAKE, FAKE, three(*ins), three(*outs))
+
+
+@pytest.mark.parametrize("outs", [(0, 4096, 128), (4096, 0, 128), (4096, 4096, 0), (4096, 4096, 64), (4096, 4096, -120), (8, 4096, 128)])
+def test_outputs_whose_rows_overlap(lib, outs):  # noqa: F811
+    """An expanded output would have its rows written by several workgroups."""
+    for x in "qkv":
+        refused(lib, INVALID, lambda: rope(lib, **{x: rows(outs=outs)}))
+        lib.fake_reset(-1)                                     # an input may repeat its rows
+        assert rope(lib, **{x: rows(ins=outs)}) == OK and lib.fake_calls() == 1
+
+
+def test_outputs_of_one_row_along_a_dimension(lib):  # noqa: F811
+    for kw, outs in ((dict(S=1), (0, 4096, 128)), (dict(n=1), (4096, 0, 128)), (dict(hkv=1), (4096, 128, 0)), (dict(), (4096, 512, -128))):
+        lib.fake_reset(-1)
+        assert rope(lib, k=rows(outs=outs), **kw) == OK and lib.fake_calls() == 1
