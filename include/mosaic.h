@@ -452,7 +452,8 @@ mosaic_status mosaic_dense_decode_attention(const void *q, const void *k, const 
  *                  [num_tokens][128] out.  v may be NULL; its rows are copied.
  *                  An output may be its own input (same pointer and strides);
  *                  otherwise nothing may overlap.  Pointers are 16-byte
- *                  aligned, strides multiples of 8.
+ *                  aligned, strides multiples of 8 (along a dimension of one
+ *                  row anything).
  *   q_weight, k_weight : [128] of the dtype, 16-byte aligned; both NULL: no
  *                  norm, rotation alone
  *   positions    : int32 (pos_bytes 4) or int64 (8) at sequence * pos_strides
@@ -511,8 +512,9 @@ typedef struct {
 /* Appends tokens to every sequence: new_lens[s] of them (DEVICE int32 [S],
  * values outside 0..max_new count as the nearest), or max_new each with NULL.
  *   k, v : rows of 128 at sequence * strides[0] + kv head * strides[1] + token *
- *          strides[2] elements (host arrays, multiples of 8), 16-byte aligned;
- *          rows from new_lens[s] on are not read
+ *          strides[2] elements (host arrays, multiples of 8, along a dimension
+ *          of one row anything), 16-byte aligned; rows from new_lens[s] on are
+ *          not read
  * The lengths are known on the device only: a sequence that has no room for all
  * of its new tokens takes none of them, and its entry of `refused` counts up.
  * Errors: INVALID, UNSUPPORTED (head_dim, block_len, max_new of 2^28 or more),

@@ -92,7 +92,11 @@ hipError_t attend(const mosaic_quant_cache *c, const QCache &qc, const void *q, 
     return f(qc, c->block_len, c->dtype, (const uint16_t *)q, scale, sel, ws, out, (hipStream_t)stream);
 }
 
-bool bad_strides(const int64_t *s) { return (s[0] | s[1] | s[2]) % 8 != 0; }
+// strides of a tensor of n0 x n1 x n2 rows that leave some row misaligned (the
+// stride of a dimension of one row may be anything)
+bool bad_strides(const int64_t *s, int n0, int n1, int n2) {
+    return ((n0 > 1 ? s[0] : 0) | (n1 > 1 ? s[1] : 0) | (n2 > 1 ? s[2] : 0)) % 8 != 0;
+}
 
 // rows of an output that share memory, along one of its dimensions
 bool rows_overlap(const int64_t *s, int n0, int n1, int n2) {
@@ -113,7 +117,8 @@ mosaic_status mosaic_quant_append(const mosaic_quant_cache *c, const void *k, co
     if (st != MOSAIC_OK) return st;
     if (!k || !v || !k_strides || !v_strides) return fail(MOSAIC_ERR_INVALID, "NULL argument");
     if (max_new < 0) return fail(MOSAIC_ERR_INVALID, "max_new %d", max_new);
-    if (off16(k) || off16(v) || bad_strides(k_strides) || bad_strides(v_strides))
+    const int S = c->num_seqs, H = c->num_kv_heads;
+    if (off16(k) || off16(v) || bad_strides(k_strides, S, H, max_new) || bad_strides(v_strides, S, H, max_new))
         return fail(MOSAIC_ERR_INVALID, "k/v must be 16-byte aligned, their strides multiples of 8 elements");
     if ((uintptr_t)new_lens % 4) return fail(MOSAIC_ERR_INVALID, "new_lens must be 4-byte aligned");
     const long long room = (long long)c->max_blocks * c->block_len;
@@ -181,9 +186,11 @@ mosaic_status mosaic_qk_norm_rope(const mosaic_rows *q, const mosaic_rows *k, co
         const mosaic_rows *r = rows[i];
         if (!r) continue;
         if (!r->in || !r->out) return fail(MOSAIC_ERR_INVALID, "NULL rows");
-        if (off16(r->in) || off16(r->out) || bad_strides(r->in_strides) || bad_strides(r->out_strides))
+        const int heads = i == 0 ? q_heads : kv_heads;
+        if (off16(r->in) || off16(r->out) || bad_strides(r->in_strides, num_seqs, num_tokens, heads) ||
+            bad_strides(r->out_strides, num_seqs, num_tokens, heads))
             return fail(MOSAIC_ERR_INVALID, "rows must be 16-byte aligned, their strides multiples of 8 elements");
-        if (rows_overlap(r->out_strides, num_seqs, num_tokens, i == 0 ? q_heads : kv_heads))
+        if (rows_overlap(r->out_strides, num_seqs, num_tokens, heads))
             return fail(MOSAIC_ERR_INVALID, "rows of an output overlap");
         (i == 0 ? a.q : (i == 1 ? a.k : a.vp)) = NormRope::Part{(const uint16_t *)r->in, (uint16_t *)r->out, r->in_strides[0], r->in_strides[1],
                                                                r->in_strides[2], r->out_strides[0], r->out_strides[1], r->out_strides[2]};

@@ -47,3 +47,17 @@ def test_outputs_whose_rows_overlap_are_refused():
             M.qk_norm_rope(x, x, pos, inv, v=x, **{name: one.expand(shape)})
     q, k = M.qk_norm_rope(x[:1, :1, :1].expand(S, n, H, D), x, pos, inv)      # an input may repeat its rows
     assert torch.equal(q, q[:1, :1, :1].expand_as(q))
+
+
+def test_one_token_with_any_stride():
+    """One token whose stride along the tokens is 1, as a transposed column has it."""
+    S, H, G = 2, 3, 2
+    x = torch.randn(S, H, D, 1, device="cuda").half()
+    c, d = (M.QuantCache(M.QuantParams(H, G, "fp16", "int8", 32), S, 64) for _ in range(2))
+    c.append(x.transpose(2, 3), x.transpose(2, 3))
+    d.append(x[..., 0], x[..., 0])
+    assert torch.equal(c.k_tail[:, :, 0], d.k_tail[:, :, 0]) and torch.equal(c.v_tail[..., 0], d.v_tail[..., 0])
+    y = torch.randn(S, D, 1, 1, device="cuda").half().permute(0, 2, 3, 1)
+    pos, inv = torch.full((S, 1), 9, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda")
+    a, b = M.qk_norm_rope(y, y, pos, inv), M.qk_norm_rope(y.reshape(S, 1, 1, D).clone(), y.reshape(S, 1, 1, D).clone(), pos, inv)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

@@ -23,3 +23,15 @@ def test_outputs_of_one_row_along_a_dimension(lib):  # noqa: F811
     for kw, outs in ((dict(S=1), (0, 4096, 128)), (dict(n=1), (4096, 0, 128)), (dict(hkv=1), (4096, 128, 0)), (dict(), (4096, 512, -128))):
         lib.fake_reset(-1)
         assert rope(lib, k=rows(outs=outs), **kw) == OK and lib.fake_calls() == 1
+
+
+def test_strides_along_one_row(lib):  # noqa: F811
+    """A dimension of one row has no alignment: its stride is not used."""
+    for kw, st in ((dict(S=1), (1, 4096, 128)), (dict(n=1), (4096, 1, 128)), (dict(hkv=1), (4096, 4096, 1))):
+        lib.fake_reset(-1)
+        assert rope(lib, k=rows(st, st), v=rows(st, st), **kw) == OK and lib.fake_calls() == 1
+        refused(lib, INVALID, lambda: rope(lib, k=rows(ins=st)))
+    for c, n, st in ((cache(num_seqs=1), 8, (1, 1024, 128)), (cache(num_kv_heads=1), 8, (8192, 1, 128)), (cache(), 1, (8192, 1024, 1))):
+        lib.fake_reset(-1)
+        assert append(lib, c, ks=three(*st), vs=three(*st), n=n) == OK and lib.fake_calls() == 1
+        refused(lib, INVALID, lambda: append(lib, cache(), ks=three(*st)))
