@@ -630,6 +630,8 @@ class QuantCache:
         taken, ascending, then -1."""
         import torch
         out = self._query(q, out)
+        if not -1 << 31 <= select[0] < 1 << 31 or not -1 << 31 <= select[1] < 1 << 31:
+            raise ValueError(f"select {select}: a share of 32-bit integers")
         if blocks is not None:
             _check_tensor(blocks, "blocks", torch.int32, self.device)
             if blocks.shape != self.k_scale.shape:

@@ -61,3 +61,13 @@ def test_one_token_with_any_stride():
     pos, inv = torch.full((S, 1), 9, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda")
     a, b = M.qk_norm_rope(y, y, pos, inv), M.qk_norm_rope(y.reshape(S, 1, 1, D).clone(), y.reshape(S, 1, 1, D).clone(), pos, inv)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_shares_past_32_bits_are_refused():
+    """(They were cut to their lower halves: another share.)"""
+    c = M.QuantCache(M.QuantParams(1, 1, "fp16", "int8", 32), 1, 64)
+    q = torch.zeros(1, 1, D, dtype=torch.float16, device="cuda")
+    for share in ((1, (1 << 32) + 10), ((1 << 32) + 1, 10), (1 << 31, 1 << 31)):
+        with pytest.raises(ValueError):
+            c.decode_selected(q, 1.0, share)
+    c.decode_selected(q, 1.0, ((1 << 31) - 1, (1 << 31) - 1))
