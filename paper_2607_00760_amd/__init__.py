@@ -525,6 +525,8 @@ class QuantCache:
         if set(given) - set(self.TENSORS):
             raise ValueError(f"unknown tensors {sorted(set(given) - set(self.TENSORS))}")
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError(f"device {device}: a GPU")
         if self.device.index is None:
             at = next((t.device for t in given.values() if isinstance(t, torch.Tensor) and t.device.type == "cuda"), None)
             self.device = at or torch.device("cuda", torch.cuda.current_device())
