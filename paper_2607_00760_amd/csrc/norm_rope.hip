@@ -173,8 +173,8 @@ hipError_t launch_norm_rope(const NormRope &a, int dtype, int interleaved, hipSt
     const int nrows = a.hq + a.hkv * (a.v ? 2 : 1), all = ceil_div(nrows, NR_ROWS);
     const long long tokens = (long long)a.seqs * a.n;
     // a token's rounds in one workgroup share its sines; with few tokens the
-    // rounds go to workgroups of their own
-    const int rounds = tokens >= 512 ? (all < NR_AHEAD ? all : NR_AHEAD) : 1;
+    // rounds go to workgroups of their own, as far as a grid's second dimension goes
+    const int rounds = tokens >= 512 || all > 65535 ? (all < NR_AHEAD ? all : NR_AHEAD) : 1;
     const dim3 grid((uint32_t)tokens, ceil_div(all, rounds));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, rounds); };
     if (dtype) {

@@ -1,6 +1,8 @@
 """Further calls of the operators around the 8-bit cache on the CPU: what is
 refused before anything is enqueued, and what is not (over the recording HIP
 runtime of tests/test_quant_args.py)."""
+import ctypes as C
+
 import pytest
 
 from test_quant_args import FAKE, INVALID, OK, _lib, append, cache, lib, refused, rope, three  # noqa: F401
@@ -35,3 +37,13 @@ def test_strides_along_one_row(lib):  # noqa: F811
         lib.fake_reset(-1)
         assert append(lib, c, ks=three(*st), vs=three(*st), n=n) == OK and lib.fake_calls() == 1
         refused(lib, INVALID, lambda: append(lib, cache(), ks=three(*st)))
+
+
+@pytest.mark.parametrize("hq,hkv", [(65535 * 16, 1), (1 << 20, 8), (1 << 20, 1 << 20), (32, 1 << 20)])
+def test_many_heads_fit_a_grid(lib, hq, hkv):  # noqa: F811
+    """A grid's second dimension holds 65535 workgroups."""
+    lib.fake_reset(-1)
+    assert rope(lib, hq=hq, hkv=hkv, v=rows(), n=1) == OK and lib.fake_calls() == 1
+    g = (C.c_uint * 3)()
+    lib.fake_call_grid(0, g)
+    assert g[0] == 2 and g[1] <= 65535 and g[2] == 1
