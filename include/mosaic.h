@@ -445,7 +445,8 @@ mosaic_status mosaic_dense_decode_attention(const void *q, const void *k, const 
  * laid out beside the keys.  The rotation turns pair i < rot_dim / 2 of
  * channels by position * inv_freq[i]: channels (i, i + rot_dim / 2), or
  * (2 i, 2 i + 1) when interleaved; channels from rot_dim on keep their place.
- * Arithmetic is fp32 (the angle's turns fp64), rounded once to the dtype.
+ * Arithmetic is fp32 (the angle's turns fp64), rounded once to the dtype; rows
+ * may be of any magnitude.
  *   q, k, v      : rows in and out with element strides {sequence, token,
  *                  head} (the 128 channels of a row are contiguous), e.g.
  *                  views of one fused projection in, [num_seqs][kv_heads]

@@ -27,6 +27,13 @@ constexpr int NR_AHEAD = 4;                                // rounds of a workgr
 template <int ROR> __device__ __forceinline__ float row_ror_add(float x) {
     return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + ROR, 0xf, 0xf, false));
 }
+// over the 16 lanes of a row: the same sum in each
+__device__ __forceinline__ float row_sum(float x) {
+    x = row_ror_add<8>(x);
+    x = row_ror_add<4>(x);
+    x = row_ror_add<2>(x);
+    return row_ror_add<1>(x);
+}
 
 // pair i of a lane's 8 channels: (i, 4 + i), or (2 i, 2 i + 1) when interleaved
 template <int DT, bool INTER> __device__ __forceinline__ float2 pair_of(const uint2 (&r)[2], int i) {
@@ -130,12 +137,22 @@ __global__ void __launch_bounds__(256) k_norm_rope(NormRope a, int rounds) {
         }
         float inv = 1.0f;
         if (norm) {
-            ss = row_ror_add<8>(ss);
-            ss = row_ror_add<4>(ss);
-            ss = row_ror_add<2>(ss);
-            ss = row_ror_add<1>(ss);
-            const float mean = ss * (1.0f / D) + a.eps;
-            const bool tiny = mean < 0x1p-96f;             // (the instruction takes no subnormal numbers)
+            float mean = row_sum(ss) * (1.0f / D) + a.eps;
+            // Squares out of fp32's range (bf16 rows only; a row's lanes agree): the
+            // row is taken 2^80 times as large, or 2^-70.  One comparison of patterns.
+            constexpr uint32_t least = 31u << 23, most = 255u << 23;           // 2^-96, infinity
+            if (DT && __float_as_uint(mean) - least >= most - least) {
+                const float by = mean < 1.0f ? 0x1p80f : 0x1p-70f;
+                ss = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f[i].x *= by;
+                    f[i].y *= by;
+                    ss = fmaf(f[i].x, f[i].x, fmaf(f[i].y, f[i].y, ss));
+                }
+                mean = row_sum(ss) * (1.0f / D) + a.eps * by * by;
+            }
+            const bool tiny = !DT && mean < 0x1p-96f;      // (zeros and a tiny eps; the instruction takes no subnormal numbers)
             inv = __builtin_amdgcn_rsqf(tiny ? mean * 0x1p64f : mean) * (tiny ? 0x1p32f : 1.0f);
         } else if (!turned) {
             return;                                        // (as they came, whatever they are)
