@@ -535,7 +535,8 @@ mosaic_status mosaic_quant_workspace_bytes(const mosaic_quant_cache *cache, size
  *   q   : [S][H * group_size][128] (cache dtype), 16-byte aligned
  *   out : [S][H * group_size][128] fp32, 16-byte aligned
  *   ws  : at least mosaic_quant_workspace_bytes bytes, 256-byte aligned
- * A sequence without tokens gets zeros.  Logits must stay within fp32. */
+ * A sequence without tokens gets zeros.  q, K and V may be of any magnitude as
+ * long as products of q, K and sm_scale stay within fp32. */
 mosaic_status mosaic_quant_decode_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,
                                             void *ws, size_t ws_bytes, void *stream);
 

@@ -434,7 +434,7 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
     [S][Hkv][n][128] and with v also v_out [S][Hkv][n][128] (v's rows as they
     are): new tensors, or the given ones, which may be views of any strides.
     An output may be its own input's memory, row for row; otherwise nothing may
-    overlap."""
+    overlap.  Outputs carry no gradient."""
     import torch
     if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k are tensors [S][n][heads][128]")
@@ -504,7 +504,8 @@ class QuantCache:
     the unfinished blocks k_tail [S][H][B][128] and v_tail [S][H][128][B], and
     lens [S][H].  tensors: a dict of these to use in place of new ones (all, or
     some).  Lengths live on the device: nothing here synchronizes, and captured
-    calls follow them.  Calls on one cache must be ordered (one stream, or
+    calls follow them.  Attention takes one query token a sequence, and outputs
+    carry no gradient.  Calls on one cache must be ordered (one stream, or
     events); they share its workspace."""
 
     TENSORS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens")

@@ -190,7 +190,12 @@ hipError_t launch_norm_rope(const NormRope &a, int dtype, int interleaved, hipSt
     const int nrows = a.hq + a.hkv * (a.v ? 2 : 1), all = ceil_div(nrows, NR_ROWS);
     const long long tokens = (long long)a.seqs * a.n;
     // a token's rounds in one workgroup share its sines; with few tokens the
-    // rounds go to workgroups of their own, as far as a grid's second dimension goes
+    // rounds go to workgroups of their own, as far as a grid's second dimension
+    // goes.  us of captured calls, one round / up to four rounds a workgroup:
+    //   tokens              16           256          512          1024         2048
+    //   48 rows (32 + 16)   3.0 / 3.9    3.8 / 4.5    5.1 / 5.2    7.7 / 6.2    12.7 / 10.1
+    //   80 rows (64 + 16)   3.0 / 4.3    4.7 / 5.1    7.0 / 5.8    11.2 / 8.5   23.8 / 18.0
+    //   24 rows (16 + 8)    3.0 / 3.5    3.4 / 3.8    4.1 / 4.1    6.2 / 5.1    9.3 / 7.7
     const int rounds = tokens >= 512 || all > 65535 ? (all < NR_AHEAD ? all : NR_AHEAD) : 1;
     const dim3 grid((uint32_t)tokens, ceil_div(all, rounds));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, rounds); };

@@ -35,15 +35,15 @@ constexpr int QA_NWV = 4;                                  // waves of a workgro
 __host__ __device__ __forceinline__ int qa_runs(int pairs) { return pairs <= 256 ? 512 - pairs : 1024; }
 // Units of a run at least: two steps a wave, and up to four rather than a
 // second workgroup on a compute unit (a step costs 0.8 us, joining a pair's
-// runs 3).  us with runs of 4 / 8 / 12 / 16 units, 8 kv heads:
-//   1 x 1500 tokens            - /  8.8 /  9.4 / 10.3
-//   1 x 4117                12.5 /  9.9 /  9.5 /  9.7  (before QA_JOIN)
-//   8 x 1500                   - / 12.3 / 11.1 / 11.6
-//   a tenth of 4 x 32785       - / 22.4 / 22.9 / 20.5
+// runs 2).  us of calls with runs of at least 4 / 8 / 12 / 16 units, 8 kv heads:
+//   1 x 1500 tokens          8.2 /  8.7 /  9.2 /  9.9
+//   1 x 4117                 9.9 /  9.6 /  9.5 /  9.6
+//   8 x 1500                12.1 / 10.8 / 10.8 / 11.3
+//   a tenth of 4 x 32785    22.3 / 20.6 / 20.6 / 20.7
 constexpr int QA_LEAST = 2 * QA_NWV, QA_FEW = 256;
-// A pair of up to 16 units is one run: 380 tokens 8.4 -> 7.4 us.  Pairs of up to
-// 256 have no more runs than are joined with one round of loads (groups of up to
-// 4 heads): 1 x 4117 tokens 9.7 -> 9.3.
+// A pair of up to 16 units is one run: 380 tokens 8.4 -> 7.4 us when that came.
+// Pairs of up to 256 have no more runs than are joined with one round of loads
+// (groups of up to 4 heads): 1 x 4117 tokens 9.7 -> 9.3 when that came.
 constexpr int QA_ALONE = 16, QA_JOIN = 16;
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and averages of the heads
@@ -203,7 +203,7 @@ __device__ __forceinline__ bool last_of(uint32_t *counter, int n, int &flag) {
 // A compute unit reads partials at about 35 bytes a ns, so many runs are joined
 // in groups first, by each group's last workgroup: runs of a group, 0 for none.
 // (59 runs of 4 heads at once took 6.8 us; one sequence of one kv head has up to
-// 504: 256 K tokens 38.4 us at once, 21.2 in groups.)
+// 511: 256 K tokens 38.4 us at once, 21 in groups.)
 __device__ __forceinline__ int qa_group(int ns) { return ns <= 32 ? 0 : (ns <= 64 ? 8 : (ns <= 256 ? 16 : 32)); }
 
 template <int FMT, int B, int DT, bool SEL>
