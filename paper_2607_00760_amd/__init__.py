@@ -478,7 +478,7 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
         raise ValueError("v_out without v")
     if S and n:
         _launch(dev, load().mosaic_qk_norm_rope, q_rows, k_rows, v_rows, S, n, hq, hkv, D, 1 if dt == torch.bfloat16 else 0,
-                qw, kw, eps, positions.data_ptr(), positions.element_size(), _pack2(*positions.stride()), inv_freq.data_ptr(),
+                qw, kw, float(eps), positions.data_ptr(), positions.element_size(), _pack2(*positions.stride()), inv_freq.data_ptr(),
                 2 * half, int(interleaved))
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
@@ -623,7 +623,7 @@ class QuantCache:
     def decode(self, q, sm_scale: float, out=None):
         """Attention over every token: q [S][H * G][128] -> fp32 [S][H * G][128]."""
         out = self._query(q, out)
-        _launch(self.device, self.lib.mosaic_quant_decode_attention, self._cp, q.data_ptr(), out.data_ptr(), sm_scale, *self._ws)
+        _launch(self.device, self.lib.mosaic_quant_decode_attention, self._cp, q.data_ptr(), out.data_ptr(), float(sm_scale), *self._ws)
         return out
 
     def decode_selected(self, q, sm_scale: float, select=(1, 10), out=None, blocks=None):
@@ -639,6 +639,6 @@ class QuantCache:
             _check_tensor(blocks, "blocks", torch.int32, self.device)
             if blocks.shape != self.k_scale.shape:
                 raise ValueError(f"blocks shape {tuple(blocks.shape)} != {tuple(self.k_scale.shape)}")
-        _launch(self.device, self.lib.mosaic_quant_select_attention, self._cp, q.data_ptr(), out.data_ptr(), sm_scale, int(select[0]),
+        _launch(self.device, self.lib.mosaic_quant_select_attention, self._cp, q.data_ptr(), out.data_ptr(), float(sm_scale), int(select[0]),
                 int(select[1]), None if blocks is None else blocks.data_ptr(), *self._ws)
         return out

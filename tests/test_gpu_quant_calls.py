@@ -1,5 +1,6 @@
 """Calls around the 8-bit cache and the norm-and-rotation pass that a program
 may make beside the ordinary ones."""
+import numpy as np
 import pytest
 import torch
 
@@ -71,3 +72,18 @@ def test_shares_past_32_bits_are_refused():
         with pytest.raises(ValueError):
             c.decode_selected(q, 1.0, share)
     c.decode_selected(q, 1.0, ((1 << 31) - 1, (1 << 31) - 1))
+
+
+def test_scales_of_other_number_types():
+    """Numbers as numpy and torch hold them, as MosaicCache.decode takes them."""
+    c = M.QuantCache(M.QuantParams(1, 1, "fp16", "int8", 32), 1, 64)
+    x = torch.randn(1, 1, 33, D, device="cuda").half()
+    c.append(x, x)
+    q = torch.randn(1, 1, D, device="cuda").half()
+    want = c.decode(q, 0.125), c.decode_selected(q, 0.125)
+    pos, inv, w = torch.ones(1, 33, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda"), torch.ones(D, device="cuda").half()
+    y = x.transpose(1, 2)
+    rope = M.qk_norm_rope(y, y, pos, inv, w, w, eps=0.25)
+    for n in (np.float32, np.float64, torch.tensor):
+        assert torch.equal(c.decode(q, n(0.125)), want[0]) and torch.equal(c.decode_selected(q, n(0.125)), want[1])
+        assert all(torch.equal(a, b) for a, b in zip(M.qk_norm_rope(y, y, pos, inv, w, w, eps=n(0.25)), rope))
