@@ -5,15 +5,15 @@
 // out = sum_t p_t v_t / sum_t p_t, p_t = exp(scale q.k_t - max), with k_t and
 // v_t their codes times their block's scale.  One pass with running maximum
 // and sum: a wave takes a block at a time, straight from memory into matrix
-// operands.  A code of either format is a value of both 16-bit types, so the
-// logits' product is of the query's type and exact.  The outputs' product is
-// fp16: the weights take part as two fp16 parts, 22 bits, in rows 0..7 and 8..15
-// of the left operand, which groups of up to 8 heads leave room for.  (A third
-// part changes no measured error, 4e-7 to 5e-7 of the outputs for 4 K tokens,
-// 7e-7 in 32 bits throughout, and takes 1 to 2 %.)  A block's value scale goes
-// into its weights; the unit of a head's sums is a power of two that follows the
-// largest product of weight and scale, so that a block is as exact as its share
-// of the output asks, however far apart the scales are.
+// operands.  A code of either format is a value of both 16-bit types: the
+// logits' product is of the query's type and exact, the outputs' is of bf16,
+// with each weight's 24 bits in three parts (its upper half, what that leaves,
+// and what is left then) in rows [part][head] of the left operand, groups of 5
+// to 8 heads with the third in a product of its own.  bf16 reaches as far down
+// as the exponential does: a block counts as exactly where its weights lie on
+// tokens whose codes are zeros.  A block's value scale goes into its weights;
+// the unit of a head's sums is a power of two that follows the largest product
+// of weight and scale, however far apart the scales are.
 //
 // The products' layouts ask for 8 tokens of one channel in a lane: values lie
 // by channel in the cache, and the rows of the first product are dealt so that
@@ -23,6 +23,8 @@
 // HBM is the bound: 256 bytes of a token, with the next block's loads out
 // while one is worked on.
 #pragma once
+#include <type_traits>
+
 #include "quant.h"
 
 namespace mosaic {
@@ -206,15 +208,25 @@ __device__ __forceinline__ bool last_of(uint32_t *counter, int n, int &flag) {
 // 511: 256 K tokens 38.4 us at once, 21 in groups.)
 __device__ __forceinline__ int qa_group(int ns) { return ns <= 32 ? 0 : (ns <= 64 ? 8 : (ns <= 256 ? 16 : 32)); }
 
-template <int FMT, int B, int DT, bool SEL>
+// what w's upper half, as bf16, leaves of it (`half`: its mask, or 0 for all of w)
+__device__ __forceinline__ float beyond(float w, uint32_t half = 0xffff0000u) { return w - __uint_as_float(__float_as_uint(w) & half); }
+// upper halves of eight values
+__device__ __forceinline__ dbf8 upper_halves(const float (&x)[8]) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_perm(__float_as_uint(x[2 * i + 1]), __float_as_uint(x[2 * i]), 0x07060302u);
+    dbf8 r;
+    __builtin_memcpy(&r, o, 16);
+    return r;
+}
+
+// GP: heads that a part's rows hold, 4 or 8
+template <int FMT, int B, int DT, bool SEL, int GP>
 __global__ void __launch_bounds__(64 * QA_NWV) __attribute__((amdgpu_waves_per_eu(2)))
 k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *arrivals, float *part, float *outp) {
     using DM = DMma<DT>;
     constexpr int NT = B / 16, TPQ = B / 4;                // tiles of 16 tokens, tokens of a lane
-    // Weights are below 2 * 2^PS units.  The second part of a weight is taken 2^LS
-    // times as large, so that both stay in fp16's normal range down to 2^-28 of that.
-    constexpr uint32_t PS = 14;
-    constexpr float LS = 2048.0f;
+    constexpr uint32_t PS = 14;                            // weights are below 2 * 2^PS units
     __shared__ __align__(16) float mrg[QA_NWV][16][D + 2];
     __shared__ int last;
     auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
@@ -226,7 +238,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     const int p = pl.s * q.H + pl.h;
     const int b0 = pl.i * pl.c, b1 = min(blocks(pl.L), b0 + pl.c), rest = min(units(pl.L), b0 + pl.c) > b1 ? pl.L % B : 0;
     const int l16 = tid & 15, q4 = (tid & 63) >> 4;
-    const int head = min(l16 & 7, q.G - 1);                // (columns past the group repeat its last head)
+    const int head = min(l16 & (GP - 1), q.G - 1);         // (columns past the group repeat its last head)
     const uint16_t *qp = query + ((uint64_t)p * q.G + head) * D;
     const int32_t *list = SEL ? sel.list + (uint64_t)p * q.N : nullptr;
     const uint64_t pb = (uint64_t)p * q.N;
@@ -279,9 +291,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             for (int e = 0; e < 4; ++e) __builtin_memcpy(&qb[e], w[e], 16);
         }
     }
-    float m_run = -INFINITY, l_run = 0.0f;                 // head l16 % 8; the sum over this lane's tokens only
+    float m_run = -INFINITY, l_run = 0.0f;                 // head l16 % GP; the sum over this lane's tokens only
     float top = 0x1p-100f;                                 // the largest product of weight and value scale so far, of head
-                                                           // l16 % 8; acc is in units of the power of two below it, / 2^PS
+                                                           // l16 % GP; acc is in units of the power of two below it, / 2^PS
     auto expo = [](float x) { return max(__float_as_uint(x) >> 23, PS + 1u); };
     auto unit = [&](float x) { return __uint_as_float((expo(x) - PS) << 23); };                // of acc
     auto per_unit = [&](float x) { return __uint_as_float((254u + PS - expo(x)) << 23); };     // its reciprocal
@@ -318,9 +330,9 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         if (!__all(grow == 1.0f)) {                        // some head's running maximum or unit moved
             float f[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {                  // grow of head (4 q4 + r) % 8
+            for (int r = 0; r < 4; ++r) {                  // grow of head (4 q4 + r) % GP
                 const float a0 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(grow), r));
-                const float a1 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(grow), 4 + r));
+                const float a1 = GP == 4 ? a0 : __int_as_float(__builtin_amdgcn_readlane(__float_as_int(grow), 4 + r));
                 f[r] = (q4 & 1) ? a1 : a0;
             }
 #pragma unroll
@@ -329,6 +341,25 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
                 for (int r = 0; r < 4; ++r) acc[ct][r] *= f[r];
         }
         return per;
+    };
+    // the left operand of tokens 8 s + [0, 8) of the lane's; with GP = 8 the third
+    // parts are an operand of their own, in the first parts' rows
+    auto split = [&](const float (&z)[NT][4], int s, float per, int l16, dbf8 &pa, dbf8 &third) {
+        const uint32_t half1 = l16 >= GP ? 0xffff0000u : 0u, half2 = l16 >= 2 * GP ? 0xffff0000u : 0u, first = l16 < GP ? ~0u : 0u;
+        float x[8], y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float w = z[2 * s + (i >> 2)][i & 3] * per;
+            if (GP == 8) {
+                const float r = beyond(w);
+                x[i] = l16 < GP ? w : r;
+                y[i] = __uint_as_float(__float_as_uint(beyond(r)) & first);
+            } else {
+                x[i] = beyond(beyond(w, half1), half2);
+            }
+        }
+        pa = upper_halves(x);
+        if (GP == 8) third = upper_halves(y);
     };
     auto consume = [&](const QStage<FMT, B> &st) {
         float z[NT][4];
@@ -342,19 +373,19 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
             }
             const float f = zs * st.ks;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) z[n][r] = a[r] * f;          // token TPQ q4 + 4 n + r, head l16 % 8
+            for (int r = 0; r < 4; ++r) z[n][r] = a[r] * f;          // token TPQ q4 + 4 n + r, head l16 % GP
         }
-        const float per = weigh(z, st.vs, st.vs, 1.0f, 0.0f), more = l16 < 8 ? 1.0f : LS, less = l16 < 8 ? 0.0f : -LS;
+        const float per = weigh(z, st.vs, st.vs, 1.0f, 0.0f);
 #pragma unroll
         for (int s = 0; s < B / 32; ++s) {
-            dhf8 pa;
+            dbf8 pa, third;
+            split(z, s, per, l16, pa, third);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {                  // the first part, or what it leaves
-                const float w = z[2 * s + (i >> 2)][i & 3] * per;
-                pa[i] = (_Float16)fmaf((float)(_Float16)w, less, w * more);
+            for (int ct = 0; ct < 8; ++ct) {
+                const dbf8 vb = codes_bf16<FMT>(st.v[ct][2 * s], st.v[ct][2 * s + 1]);
+                acc[ct] = DMma<1>::run(pa, vb, acc[ct]);
+                if (GP == 8) acc[ct] = DMma<1>::run(third, vb, acc[ct]);
             }
-#pragma unroll
-            for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, codes_f16<FMT>(st.v[ct][2 * s], st.v[ct][2 * s + 1]), acc[ct]);
         }
     };
     while (t < b1) {                                       // (two steps a turn: no copies that would wait on the loads)
@@ -372,11 +403,10 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     }
     if (rest && wave == ((b1 - b0) & (QA_NWV - 1))) {      // the unfinished block, in 16 bits
         using M8 = typename DM::v8;
-        using E = typename DM::el;
         int at = tid;                                      // (worked out again: nothing of it lives through the loop)
         asm volatile("" : "+v"(at));
         const int l16 = at & 15, q4 = (at & 63) >> 4;
-        const uint16_t *qp = query + ((uint64_t)p * q.G + min(l16 & 7, q.G - 1)) * D;
+        const uint16_t *qp = query + ((uint64_t)p * q.G + min(l16 & (GP - 1), q.G - 1)) * D;
         const uint16_t *kp = q.kt + (uint64_t)p * B * D, *vp = q.vt + (uint64_t)p * B * D;
         M8 qd[4];
 #pragma unroll
@@ -428,21 +458,28 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         const float per = DT ? weigh(z, 1.0f, reach, 0x1p-60f, 0x1p-60f) : weigh(z, 1.0f, 1.0f, 1.0f, 0.0f);
 #pragma unroll
         for (int s = 0; s < B / 32; ++s) {
-            M8 pa, pl2{};                                  // bf16: a third part, its rows the first eight
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float w = z[2 * s + (i >> 2)][i & 3] * per;
-                const E hi = (E)w;
-                const float r1 = w - (float)hi;
-                const E mid = (E)(r1 * LS);
-                pa[i] = l16 < 8 ? hi : mid;
-                if (DT) pl2[i] = l16 < 8 ? (E)(r1 - (float)mid * (1.0f / LS)) : (E)0.0f;
-            }
+            dbf8 pa, third;
+            split(z, s, per, l16, pa, third);
+            auto add = [&](df4 &a, const dbf8 &vb) {
+                a = DMma<1>::run(pa, vb, a);
+                if (GP == 8) a = DMma<1>::run(third, vb, a);
+            };
 #pragma unroll
             for (int ct = 0; ct < 8; ++ct) {
-                const M8 vb = __builtin_bit_cast(M8, vt[s][ct]);
-                acc[ct] = DM::run(pa, vb, acc[ct]);
-                if (DT) acc[ct] = DM::run(pl2, vb, acc[ct]);
+                if (DT) {
+                    add(acc[ct], __builtin_bit_cast(dbf8, vt[s][ct]));
+                } else {                                   // an fp16 value's 11 bits in two parts
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t w = ((const uint32_t *)&vt[s][ct])[i >> 1];
+                        x[i] = h2f((uint16_t)((i & 1) ? w >> 16 : w), 0);
+                    }
+                    add(acc[ct], upper_halves(x));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = beyond(x[i]);
+                    add(acc[ct], upper_halves(x));
+                }
             }
         }
     }
@@ -453,7 +490,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     lane &= 63;
     const int row = lane >> 4, col = lane & 15;   // (worked out again, as above)
     if (lane < 16) {                                       // a head's unit stands in the row of its second parts
-        mrg[wave][col][0] = lane < 8 ? m_run : unit(top);
+        mrg[wave][col][0] = lane < GP ? m_run : unit(top);
         mrg[wave][col][1] = l_run;
     }
 #pragma unroll
@@ -479,10 +516,16 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
         const float inv = share_of(S);
 #pragma unroll
         for (int w = 0; w < QA_NWV; ++w) {
-            const float2 u = *(const float2 *)&mrg[w][h][2 + c], v = *(const float2 *)&mrg[w][h + 8][2 + c];
-            const float fu = f[w] * inv * mrg[w][h + 8][0];
-            A.x += fmaf(v.x, 1.0f / LS, u.x) * fu;
-            A.y += fmaf(v.y, 1.0f / LS, u.y) * fu;
+            const float fu = f[w] * inv * mrg[w][h + GP][0];
+            float2 u = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int e = GP == 4 ? 2 : 1; e >= 0; --e) {   // the parts, from the least
+                const float2 v = *(const float2 *)&mrg[w][h + GP * e][2 + c];
+                u.x += v.x;
+                u.y += v.y;
+            }
+            A.x += u.x * fu;
+            A.y += u.y * fu;
         }
         if (pl.ns == 1) {
             *(float2 *)(out + i) = A;
@@ -527,13 +570,14 @@ hipError_t launch_quant_attn_t(const QCache &q, int block, int dtype, const uint
     const long long most = (long long)pairs * ceil_div(units, QA_LEAST);
     const dim3 grid((uint32_t)(most < runs ? most : runs));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * QA_NWV), 0, s, q, sel, query, scale, arrivals, part, out); };
-    if (sel.list) {
-        if (block == 32) { if (dtype) go(k_quant_attn<FMT, 32, 1, true>); else go(k_quant_attn<FMT, 32, 0, true>); }
-        else { if (dtype) go(k_quant_attn<FMT, 64, 1, true>); else go(k_quant_attn<FMT, 64, 0, true>); }
-    } else {
-        if (block == 32) { if (dtype) go(k_quant_attn<FMT, 32, 1, false>); else go(k_quant_attn<FMT, 32, 0, false>); }
-        else { if (dtype) go(k_quant_attn<FMT, 64, 1, false>); else go(k_quant_attn<FMT, 64, 0, false>); }
-    }
+    auto by_group = [&](auto b, auto dt, auto selected) {
+        constexpr int BL = decltype(b)::value, T = decltype(dt)::value;
+        constexpr bool SL = decltype(selected)::value;
+        if (q.G <= 4) go(k_quant_attn<FMT, BL, T, SL, 4>); else go(k_quant_attn<FMT, BL, T, SL, 8>);
+    };
+    auto by_list = [&](auto b, auto dt) { if (sel.list) by_group(b, dt, std::true_type{}); else by_group(b, dt, std::false_type{}); };
+    auto by_type = [&](auto b) { if (dtype) by_list(b, std::integral_constant<int, 1>{}); else by_list(b, std::integral_constant<int, 0>{}); };
+    if (block == 32) by_type(std::integral_constant<int, 32>{}); else by_type(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 

@@ -108,6 +108,28 @@ def test_unfinished_block_of_mixed_values(fmt, dtype, block):
 
 
 @pytest.mark.parametrize("fmt,dtype,block", FORMS)
+@pytest.mark.parametrize("G", [2, 4, 7])
+def test_weights_on_zeros(fmt, dtype, block, G):
+    """The softmax's weight lies on tokens whose values, or codes, are zeros: the
+    output is what the others bring, 2^20 to 2^110 below their values."""
+    dt = DT[dtype]
+    g = torch.Generator().manual_seed(G)
+    u = torch.sign(torch.randn(D, generator=g))
+    unit = math.log(2.0) / (2 * SCALE * D)
+    a = torch.tensor([20.0, 35.0, 50.0, 65.0, 80.0, 95.0, 110.0][-G:]) * unit
+    q = (a[:, None] * u).to(dt)
+    for n in (block - 5, 2 * block, 41 * block + 17):
+        none = torch.rand(n, generator=g) < 0.3
+        none[0], none[-1] = True, False
+        for small in (0.0, 2.0 ** -20):                        # (codes of zero next to the block's others)
+            v = torch.randn(n, D, generator=g) * torch.where(none, small, 1.0)[:, None]
+            if small and n % block:
+                v[none & (torch.arange(n) >= n // block * block)] = 0.0
+            k = u * torch.where(none, 1.0, -1.0)[:, None]
+            check(make(fmt, dtype, block, 1, 1, G, n), k.to(dt)[None], v.to(dt)[None], q, G, f"{n} tokens, {small}")
+
+
+@pytest.mark.parametrize("fmt,dtype,block", FORMS)
 @pytest.mark.parametrize("nb,tail", [(0, 1), (0, 5), (1, 0), (9, 31), (70, 3), (700, 1)])
 def test_values_next_to_the_largest(fmt, dtype, block, nb, tail):
     """Channels of one sign at the type's largest: an average of them is finite
