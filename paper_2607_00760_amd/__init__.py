@@ -576,8 +576,11 @@ class QuantCache:
             seqs = sorted({int(s) for s in seqs})
             if seqs and not 0 <= seqs[0] <= seqs[-1] < self.num_seqs:
                 raise ValueError(f"sequences {seqs} of {self.num_seqs}")
-            for s in seqs:                                     # (nothing is copied: a graph can record it)
-                self.lens[s].zero_()
+            for i, s in enumerate(seqs):                       # a fill for each run of indices: nothing is copied, a graph
+                if i == 0 or s != seqs[i - 1] + 1:             # can record it
+                    first = s
+                if i + 1 == len(seqs) or seqs[i + 1] != s + 1:
+                    self.lens[first: s + 1].zero_()
             return
         if seqs.dtype not in (torch.int32, torch.int64) or seqs.device != self.device or seqs.dim() != 1:
             raise ValueError("seqs must be a list of indices or a one-dimensional integer tensor on the cache's GPU")

@@ -38,6 +38,18 @@ def test_reset_of_a_list_is_captured():
         assert torch.equal(c.k_tail[1, :, :2], x[1, :, :2])
 
 
+def test_reset_of_lists_of_all_kinds():
+    S, H = 9, 2
+    c = M.QuantCache(M.QuantParams(H, 1, "fp16", "int8", 32), S, 32)
+    for named in ([0], [8], [0, 8], [2, 1, 3], [0, 1, 2, 4, 5, 7], list(range(9)), (3, 3), range(4, 9), np.array([6, 0]), {5}):
+        c.lens.fill_(7)
+        c.reset(named)
+        assert c.lens.tolist() == [[0 if s in list(named) else 7] * H for s in range(S)], named
+    for bad in ([9], [0, -1], [-9, 3], [2, 100]):
+        with pytest.raises(ValueError):
+            c.reset(bad)
+
+
 def test_outputs_whose_rows_overlap_are_refused():
     S, n, H = 2, 3, 4
     x = torch.randn(S, n, H, D, device="cuda").half()
