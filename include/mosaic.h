@@ -536,7 +536,8 @@ mosaic_status mosaic_quant_workspace_bytes(const mosaic_quant_cache *cache, size
  *   out : [S][H * group_size][128] fp32, 16-byte aligned
  *   ws  : at least mosaic_quant_workspace_bytes bytes, 256-byte aligned
  * A sequence without tokens gets zeros.  q, K and V may be of any magnitude as
- * long as products of q, K and sm_scale stay within fp32. */
+ * long as products of q, K and sm_scale stay within fp32; softmax weights below
+ * 2^-126 of a head's largest count as zero. */
 mosaic_status mosaic_quant_decode_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,
                                             void *ws, size_t ws_bytes, void *stream);
 

@@ -262,7 +262,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     auto block_at = [&](int u) { return SEL ? list[min(u, b1 - 1)] : min(u, b1 - 1); };
     int id0 = 0, id1 = 0;
     if (t < b1) { id0 = block_at(t); id1 = block_at(t + QA_NWV); }
-    // q operand: column l16 is head l16 % 8, inner index (j, half, q4, i) channel 64 j + 16 q4 + 8 half + i
+    // q operand: column l16 is head l16 % GP, inner index (j, half, q4, i) channel 64 j + 16 q4 + 8 half + i
     typename DM::v8 qb[4];
     float zs = scale * 1.44269504088896340736f;            // softmax scale in powers of two, and q's
     {
