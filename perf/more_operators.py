@@ -14,11 +14,11 @@
 Plain forms compute in 32 bits from the same definitions, with elementary
 torch operations; `exact` does so in 64 bits, apart from them.
 
-Definitions.  T is the cache's 16-bit type, LEAST 2^-24 (fp16) or 2^-100
+Definitions.  T is the cache's 16-bit type, LEAST 2^-19 (fp16) or 2^-100
 (bf16).  The grid of a row x of values: lo and hi its least and largest, scale
-= the least value of T that is not below (hi / 2 - lo / 2) / 7.5 and LEAST,
-zero = lo; a value's code = nearest((x / 2 - lo / 2) * (2 / scale)), 0 to 15,
-each step in 32 bits; it stands for zero + scale * code.  Whole blocks of B
+= the largest value of T that is not above (hi / 2 - lo / 2) / 7.5, or LEAST
+where that is more, zero = lo; a value's code = nearest((x / 2 - lo / 2) * (2 /
+scale)), 0 to 15, each step in 32 bits; it stands for zero + scale * code.  Whole blocks of B
 tokens of one (sequence, kv head) are encoded: a row is a channel's keys over
 the block's tokens, or a token's values over the channels.  Tokens past the
 last whole block stay in 16 bits, in the tail.  What is read back is rounded
@@ -331,7 +331,7 @@ def _plain_axes(q, k, v, positions, inv_freq, q_weight, k_weight, interleaved, a
 
 
 def _least(dtype):
-    return 2.0 ** -100 if dtype == torch.bfloat16 else 2.0 ** -24
+    return 2.0 ** -100 if dtype == torch.bfloat16 else 2.0 ** -19
 
 
 def _grid(x, dim):
@@ -340,8 +340,8 @@ def _grid(x, dim):
     lo, hi = x.amin(dim, keepdim=True), x.amax(dim, keepdim=True)
     want = (hi * 0.5 - lo * 0.5) / torch.full_like(lo, 7.5)    # (a quotient of tensors: plain numbers divide through a reciprocal)
     scale = want.to(dt)
-    up = (scale.view(torch.int16) + 1).view(dt)                # the next value of the type
-    scale = torch.where(scale.float() < want, up, scale).float().clamp_min(_least(dt))
+    down = (scale.view(torch.int16) - 1).view(dt)              # the value of the type below it
+    scale = torch.where(scale.float() > want, down, scale).float().clamp_min(_least(dt))
     code = ((x * 0.5 - lo * 0.5) * (torch.full_like(scale, 2.0) / scale)).round()
     return code.to(torch.uint8), scale.to(dt).squeeze(dim), lo.to(dt).squeeze(dim)
 
@@ -505,7 +505,7 @@ def _stand_for(x, dt, dim):
     e = torch.floor(torch.log2(want.clamp(min=2.0 ** -140)))
     e = torch.where(torch.exp2(e) > want, e - 1, e)
     step = torch.exp2(e - 7) if dt == torch.bfloat16 else torch.exp2((e - 10).clamp(min=-24))
-    scale = (torch.ceil(want / step) * step).clamp(min=2.0 ** -100 if dt == torch.bfloat16 else 2.0 ** -24)
+    scale = (torch.floor(want / step) * step).clamp(min=2.0 ** -100 if dt == torch.bfloat16 else 2.0 ** -19)
     code = torch.round(_f32(_f32(x / 2 - lo / 2) * _f32(2.0 / scale)))
     return lo + scale * code, scale, lo
 
