@@ -115,8 +115,9 @@ def algorithmic_bytes(cache, spec, nb_list, sel_list, desc_list):
 
 
 # sources of the other paths' kernels; every other file of csrc takes part in the decode step
-OTHER_SOURCES = ("compress.hip", "dense.hip", "encode.hip", "norm_rope.h", "norm_rope.hip", "quant.h", "quant_api.hip",
-                 "quant_append.hip", "quant_attn.h", "quant_attn_e4m3.hip", "quant_attn_int8.hip", "quant_select.hip", "rotation.hip")
+OTHER_SOURCES = ("compress.hip", "dense.hip", "encode.hip", "norm_rope.h", "norm_rope.hip", "quant.h", "quant4.h",
+                 "quant4_append.hip", "quant4_attn.hip", "quant4_chunk.hip", "quant_api.hip", "quant_append.hip", "quant_attn.h",
+                 "quant_attn_e4m3.hip", "quant_attn_int8.hip", "quant_join.h", "quant_read.hip", "quant_select.hip", "rotation.hip")
 
 
 def source_hash():

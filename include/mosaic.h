@@ -477,6 +477,21 @@ mosaic_status mosaic_qk_norm_rope(const mosaic_rows *q, const mosaic_rows *k, co
                                   int32_t pos_bytes, const int64_t *pos_strides_host, const float *inv_freq,
                                   int32_t rot_dim, int32_t interleaved, void *stream);
 
+/* The same with positions of several axes (time, height and width of an image's
+ * or a video's patches): pair i turns by the position on axis axes_host[i] times
+ * inv_freq[i].
+ *   positions    : at axis * pos_strides[0] + sequence * pos_strides[1] + token *
+ *                  pos_strides[2] elements (0: shared)
+ *   axes_host    : [rot_dim / 2] host bytes below num_axes, in any order (read
+ *                  during the call)
+ * Errors also: INVALID (num_axes outside 1..255, an axis past them). */
+mosaic_status mosaic_qk_norm_rope_axes(const mosaic_rows *q, const mosaic_rows *k, const mosaic_rows *v, int32_t num_seqs,
+                                       int32_t num_tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t dtype,
+                                       const void *q_weight, const void *k_weight, float eps, const void *positions,
+                                       int32_t pos_bytes, const int64_t *pos_strides_host, const float *inv_freq,
+                                       int32_t rot_dim, int32_t interleaved, int32_t num_axes, const uint8_t *axes_host,
+                                       void *stream);
+
 /* A KV cache in 8 bits with one scale for each block of block_len tokens of a
  * (sequence, kv head), K and V apart.  For a block x of tokens x 128 channels:
  * a = max(max |x|, 2^-100), scale = a / Q, code = nearest(x * (Q / a)), ties to
@@ -554,6 +569,101 @@ mosaic_status mosaic_quant_decode_attention(const mosaic_quant_cache *cache, con
 mosaic_status mosaic_quant_select_attention(const mosaic_quant_cache *cache, const void *q, float *out, float sm_scale,
                                             int32_t select_num, int32_t select_den, int32_t *blocks, void *ws,
                                             size_t ws_bytes, void *stream);
+
+/* Tokens of the cache read back, in its dtype: codes times their scale in fp32,
+ * rounded once; the unfinished block's tokens as they came.  Row i of sequence s
+ * is its token starts[s] + i (DEVICE int32 [S], or `start` for all with NULL;
+ * may be negative), i < num_tokens.  Rows of tokens that a sequence does not
+ * hold are left as they were.
+ *   k, v : rows of 128 at sequence * strides[0] + kv head * strides[1] + token *
+ *          strides[2] elements (host arrays, multiples of 8, along a dimension
+ *          of one row anything), 16-byte aligned; rows do not overlap
+ * Errors: INVALID, UNSUPPORTED (more than 2^23 blocks). */
+mosaic_status mosaic_quant_read(const mosaic_quant_cache *cache, void *k, void *v, const int64_t *k_strides_host,
+                                const int64_t *v_strides_host, const int32_t *starts, int32_t start, int32_t num_tokens,
+                                void *stream);
+
+/* A KV cache in 4 bits.  A block of block_len tokens of a (sequence, kv head) is
+ * encoded by rows: a channel's keys over the block's tokens, and a token's
+ * values over the channels.  For a row x with least and largest value lo and hi:
+ * scale = the largest value of the dtype that is not above (hi / 2 - lo / 2) /
+ * 7.5, at least 2^-19 (fp16) or 2^-100 (bf16); zero = lo; code = nearest((x / 2 -
+ * lo / 2) * (2 / scale)), 0 to 15, ties to even, each step in fp32.  A code
+ * stands for zero + scale * code, half a scale from its value at most.  A block
+ * is encoded once, when its last token arrives; until then its tokens are kept
+ * in 16 bits (the tail), so a cache's contents depend on its tokens and not on
+ * the calls that brought them.  A row with a value that is not finite stands for
+ * NaN.
+ *
+ * The caller owns every array; all are contiguous.  S = num_seqs, H =
+ * num_kv_heads, N = max_blocks, B = block_len (32 or 64); room is N B tokens a
+ * sequence.  lens must start at zero; setting a sequence's entries to zero (or
+ * all of them) empties it.  What lies behind a sequence's last block or token
+ * takes part in nothing, whatever it holds, and is left as it was.  K and V must
+ * be finite; a value that is not spoils its own (sequence, kv head) only. */
+typedef struct {
+    int32_t num_seqs, num_kv_heads, group_size, head_dim;  /* head_dim 128, group_size 1..8 */
+    int32_t dtype;                     /* mosaic_dtype of tokens, grids, tails and queries */
+    int32_t block_len, max_blocks;
+    int32_t reserved;                  /* 0 */
+    void *k;                           /* codes [S][H][N][B][64]: byte i holds channels 2 i (lower half) and 2 i + 1 */
+    void *v;                           /* codes [S][H][N][128][B / 2] (by channel): byte i holds tokens 2 i and 2 i + 1 */
+    void *k_grid;                      /* [S][H][N][2][128] of the dtype: scales of the channels, zeros */
+    void *v_grid;                      /* [S][H][N][2][B] of the dtype: scales of the tokens, zeros */
+    void *k_tail;                      /* [S][H][B][128] of the dtype */
+    void *v_tail;                      /* [S][H][128][B] of the dtype; all of these 16-byte aligned */
+    int32_t *lens;                     /* [S][H] tokens held (a sequence's entries are equal) */
+    int32_t *arrivals;                 /* [S][H][32] the library's own; zero before the first append */
+    int32_t *refused;                  /* [S] appends that a sequence had no room for */
+} mosaic_nibble_cache;
+
+/* As mosaic_quant_append and mosaic_quant_read; what is read back is zero +
+ * scale * code in fp32, rounded once to the dtype. */
+mosaic_status mosaic_nibble_append(const mosaic_nibble_cache *cache, const void *k, const void *v,
+                                   const int64_t *k_strides_host, const int64_t *v_strides_host, const int32_t *new_lens,
+                                   int32_t max_new, void *stream);
+mosaic_status mosaic_nibble_read(const mosaic_nibble_cache *cache, void *k, void *v, const int64_t *k_strides_host,
+                                 const int64_t *v_strides_host, const int32_t *starts, int32_t start, int32_t num_tokens,
+                                 void *stream);
+
+/* Workspace of the two attentions below (depends on the cache's shape only).
+ * Its first 512 KiB must be zero before its first use; every call leaves them
+ * so, and caches of other shapes may use it in turn if it is large enough.
+ * Calls that overlap on one workspace race; separate streams need their own. */
+mosaic_status mosaic_nibble_workspace_bytes(const mosaic_nibble_cache *cache, size_t *bytes);
+
+/* Decode attention over every token of the cache, one query token a sequence:
+ * over the numbers that the codes stand for (not rounded), and the tail.
+ *   q   : [S][H * group_size][128] (cache dtype), 16-byte aligned
+ *   out : [S][H * group_size][128] fp32, 16-byte aligned
+ *   ws  : at least mosaic_nibble_workspace_bytes bytes, 256-byte aligned
+ * A sequence without tokens gets zeros.  V may be of any magnitude, q and K as
+ * long as a head's products of q with scales and zeros, and their sums times
+ * sm_scale, stay within fp32; softmax weights below 2^-126 of a head's largest
+ * count as zero. */
+mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *cache, const void *q, float *out, float sm_scale,
+                                             void *ws, size_t ws_bytes, void *stream);
+
+/* Attention of several query tokens of each sequence over the tokens as
+ * mosaic_nibble_read gives them: sequence s has m = new_lens[s] of them (DEVICE
+ * int32 [S], values outside 0..max_new count as the nearest), or max_new each
+ * with NULL.  causal: query i is the sequence's token L - m + i (its keys and
+ * values are in the cache) and attends the tokens up to it; otherwise every
+ * query attends every token.
+ *   q, out : rows of 128 (cache dtype) at sequence * strides[0] + query token *
+ *            strides[1] + head * strides[2] elements (host arrays, multiples of
+ *            8, along a dimension of one row anything), 16-byte aligned; rows
+ *            from new_lens[s] on are neither read nor written; out's rows do not
+ *            overlap, out may be q (same pointer and strides)
+ *   ws     : at least mosaic_nibble_workspace_bytes bytes, 256-byte aligned
+ * Softmax weights are rounded to the dtype before their product with V.  A query
+ * that attends nothing gets zeros.  q, K and V as long as a head's products and
+ * the sums of weights times values stay within fp32.
+ * Errors: INVALID, UNSUPPORTED (head_dim, block_len, max_new past 2^27 or 2^23
+ * tiles of 32 rows). */
+mosaic_status mosaic_nibble_attend(const mosaic_nibble_cache *cache, const void *q, void *out, const int64_t *q_strides_host,
+                                   const int64_t *out_strides_host, const int32_t *new_lens, int32_t max_new, int32_t causal,
+                                   float sm_scale, void *ws, size_t ws_bytes, void *stream);
 
 /* Memory accounting of Sec. 6.3 (reads the device state: synchronizes the
  * given stream).  used_bytes counts packed tokens, block keys, descriptors

@@ -12,9 +12,10 @@ import struct
 from dataclasses import dataclass
 
 from ._lib import (OP_APPEND, OP_COMPRESS, OP_DECODE, OP_WINDOW_ROTATIONS, MosaicError, MosaicLayout, MosaicParams,
-                   MosaicQuantCache, MosaicStats, MosaicWsLayout, check, load)
+                   MosaicNibbleCache, MosaicQuantCache, MosaicStats, MosaicWsLayout, check, load)
 
-__all__ = ["Params", "MosaicCache", "QuantParams", "QuantCache", "dense_decode", "qk_norm_rope", "MosaicError", "load"]
+__all__ = ["Params", "MosaicCache", "QuantParams", "QuantCache", "Quant4Params", "Quant4Cache", "dense_decode", "qk_norm_rope",
+           "MosaicError", "load"]
 
 D = 128
 # argument structures as bytes: a third of the time of ctypes' own
@@ -421,7 +422,7 @@ def _vector(t, name, dtype, device):
 
 
 def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, v=None,
-                 q_out=None, k_out=None, v_out=None):
+                 q_out=None, k_out=None, v_out=None, axes=None):
     """Norm of each query and key head (with weights) and rotation to the
     tokens' positions, in one pass, laid out for the caches.
 
@@ -433,6 +434,8 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
     k_weight [128] or neither.  Returns q_out [S][n][Hq][128], k_out
     [S][Hkv][n][128] and with v also v_out [S][Hkv][n][128] (v's rows as they
     are): new tensors, or the given ones, which may be views of any strides.
+    axes: positions have several axes (time, height, width), [A][S][n], and
+    axes[i] (R / 2 integers, or bytes) is the one whose position turns pair i.
     An output may be its own input's memory, row for row; otherwise nothing may
     overlap.  Outputs carry no gradient."""
     import torch
@@ -447,11 +450,23 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
     hkv = k.shape[2]
     if not isinstance(positions, torch.Tensor) or positions.dtype not in (torch.int32, torch.int64):
         raise ValueError("positions must be an int32 or int64 tensor")
-    if positions.device != dev or positions.shape != (S, n):
-        raise ValueError(f"positions: shape {tuple(positions.shape)} on {positions.device}, expected {(S, n)} on {dev}")
+    at = positions.shape
+    if axes is not None and positions.dim() == 3:
+        at = at[1:]
+    if positions.device != dev or at != (S, n):
+        raise ValueError(f"positions: shape {tuple(positions.shape)} on {positions.device}, expected "
+                         f"{(S, n) if axes is None else ('axes', S, n)} on {dev}")
     if (q_weight is None) != (k_weight is None):
         raise ValueError("give both weights or neither")
     half = _vector(inv_freq, "inv_freq", torch.float32, dev)
+    call, last, strides = load().mosaic_qk_norm_rope, (), positions.stride()
+    if axes is not None:
+        if positions.dim() != 3 or not 1 <= positions.shape[0] <= 255:
+            raise ValueError(f"positions: shape {tuple(positions.shape)}, expected (axes, {S}, {n}) with 1 to 255 axes")
+        axes = bytes(axes) if isinstance(axes, (bytes, tuple, list)) else bytes(int(i) for i in axes)
+        if len(axes) != half or (half and max(axes) >= positions.shape[0]):
+            raise ValueError(f"axes: {len(axes)} of values up to {max(axes, default=0)}, expected {half} below {positions.shape[0]}")
+        call, last = load().mosaic_qk_norm_rope_axes, (positions.shape[0], axes)
     qw = kw = None
     if q_weight is not None:
         if _vector(q_weight, "q_weight", dt, dev) != D or _vector(k_weight, "k_weight", dt, dev) != D:
@@ -477,52 +492,30 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
     elif v_out is not None:
         raise ValueError("v_out without v")
     if S and n:
-        _launch(dev, load().mosaic_qk_norm_rope, q_rows, k_rows, v_rows, S, n, hq, hkv, D, 1 if dt == torch.bfloat16 else 0,
-                qw, kw, float(eps), positions.data_ptr(), positions.element_size(), _pack2(*positions.stride()), inv_freq.data_ptr(),
-                2 * half, int(interleaved))
+        _launch(dev, call, q_rows, k_rows, v_rows, S, n, hq, hkv, D, 1 if dt == torch.bfloat16 else 0, qw, kw, float(eps),
+                positions.data_ptr(), positions.element_size(), _pack3(*strides) if last else _pack2(*strides), inv_freq.data_ptr(),
+                2 * half, int(interleaved), *last)
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 
-@dataclass
-class QuantParams:
-    """Shape of an 8-bit cache: codes ("e4m3" or "int8") with one scale for each
-    block of `block` (32 or 64) tokens and kv head."""
-    num_kv_heads: int = 8
-    group_size: int = 4
-    dtype: str = "fp16"
-    format: str = "e4m3"
-    block: int = 32
+class _BlockCache:
+    """What the caches of encoded blocks have in common: their calls take
+    _append, _read and _decode of the library, and the structure _c."""
 
+    TENSORS = ()
 
-class QuantCache:
-    """One layer's KV cache in 8 bits for `num_seqs` sequences of up to
-    max_tokens tokens (rounded up to whole blocks).
-
-    The cache is its tensors (attributes; S sequences, H kv heads, N blocks of B
-    tokens): codes k [S][H][N][B][128] and v [S][H][N][128][B], k_scale, v_scale
-    and bound_scale [S][H][N], bounds [S][H][N][2][128], the 16-bit tokens of
-    the unfinished blocks k_tail [S][H][B][128] and v_tail [S][H][128][B], and
-    lens [S][H].  tensors: a dict of these to use in place of new ones (all, or
-    some).  Lengths live on the device: nothing here synchronizes, and captured
-    calls follow them.  Attention takes one query token a sequence, and outputs
-    carry no gradient.  Calls on one cache must be ordered (one stream, or
-    events); they share its workspace."""
-
-    TENSORS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens")
-
-    def __init__(self, params: QuantParams, num_seqs: int, max_tokens: int, device="cuda", tensors=None):
+    def _make(self, params, num_seqs, max_tokens, device, given):
+        """Checks what the parameters of both have in common; the device is the
+        given tensors', or the current one, unless it says more."""
         import torch
         self.lib = load()
         self.params, self.num_seqs = params, num_seqs
         if params.dtype not in ("fp16", "bf16"):
             raise ValueError(f"dtype {params.dtype!r}: fp16 or bf16")
-        if params.format not in ("e4m3", "int8"):
-            raise ValueError(f"format {params.format!r}: e4m3 or int8")
         if params.block not in (32, 64):
             raise ValueError(f"block {params.block}: 32 or 64")
         if num_seqs < 1 or max_tokens < 1:
             raise ValueError(f"num_seqs {num_seqs}, max_tokens {max_tokens}")
-        given = dict(tensors or {})
         if set(given) - set(self.TENSORS):
             raise ValueError(f"unknown tensors {sorted(set(given) - set(self.TENSORS))}")
         self.device = torch.device(device)
@@ -532,16 +525,15 @@ class QuantCache:
             at = next((t.device for t in given.values() if isinstance(t, torch.Tensor) and t.device.type == "cuda"), None)
             self.device = at or torch.device("cuda", torch.cuda.current_device())
         self.elem = torch.bfloat16 if params.dtype == "bf16" else torch.float16
-        S, H, B, N = num_seqs, params.num_kv_heads, params.block, -(-max_tokens // params.block)
-        self.max_tokens = N * B
-        code = torch.int8 if params.format == "int8" else torch.float8_e4m3fn
-        shapes = dict(k=((N, B, D), code), v=((N, D, B), code), k_scale=((N,), torch.float32), v_scale=((N,), torch.float32),
-                      bound_scale=((N,), torch.float32), bounds=((N, 2, D), torch.int8), k_tail=((B, D), self.elem),
-                      v_tail=((D, B), self.elem), lens=((), torch.int32))
-        self._c = MosaicQuantCache(S, H, params.group_size, D, 1 if params.dtype == "bf16" else 0, 1 if params.format == "int8" else 0,
-                                   B, N)
+        self.max_tokens = -(-max_tokens // params.block) * params.block
+
+    def _take(self, c, shapes, given, ws_bytes):
+        """The tensors (those given, or new ones) and the rest of the structure."""
+        import torch
+        self._c = c
+        S, H = self.num_seqs, self.params.num_kv_heads
         n = C.c_size_t()
-        check(self.lib.mosaic_quant_workspace_bytes(C.byref(self._c), C.byref(n)))
+        check(ws_bytes(C.byref(c), C.byref(n)))
         for name, (tail, dtype) in shapes.items():
             t = given.get(name)
             if t is None:
@@ -551,16 +543,16 @@ class QuantCache:
             if tuple(t.shape) != (S, H) + tail:
                 raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(S, H) + tail}")
             setattr(self, name, t)
-            setattr(self._c, name, t.data_ptr())
+            setattr(c, name, t.data_ptr())
         #: appends that each sequence had no room for (it took none of their tokens)
         self.refused = torch.zeros(S, dtype=torch.int32, device=self.device)
-        self._c.refused = self.refused.data_ptr()
+        c.refused = self.refused.data_ptr()
         self._arrivals = torch.zeros((S, H, 32), dtype=torch.int32, device=self.device)
-        self._c.arrivals = self._arrivals.data_ptr()
+        c.arrivals = self._arrivals.data_ptr()
         self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=self.device)
-        self._cp = C.byref(self._c)
+        self._cp = C.byref(c)
         self._ws = (self.workspace.data_ptr(), n.value)
-        self._q_shape = (S, H * params.group_size, D)
+        self._q_shape = (S, H * self.params.group_size, D)
 
     def tensors(self) -> dict:
         return {n: getattr(self, n) for n in self.TENSORS}
@@ -606,9 +598,37 @@ class QuantCache:
                 raise ValueError(f"new_lens has shape {tuple(new_lens.shape)}, expected {(S,)}")
         if shape[2] == 0:
             return
-        _launch(self.device, self.lib.mosaic_quant_append, self._cp, k.data_ptr(), v.data_ptr(), _pack3(*ks[:3]), _pack3(*vs[:3]),
+        _launch(self.device, self._append, self._cp, k.data_ptr(), v.data_ptr(), _pack3(*ks[:3]), _pack3(*vs[:3]),
                 None if new_lens is None else new_lens.data_ptr(), shape[2])
         self._keep = (k, v, new_lens)  # alive until the enqueued work completes
+
+    def read(self, n: int, start=0, k_out=None, v_out=None):
+        """Tokens start to start + n - 1 of every sequence in 16 bits, as the
+        codes stand for them: k, v [S][H][n][128], new or the given ones (any
+        strides with contiguous channels).  start: an integer, or int32 [S] on
+        the GPU; it may be negative.  Rows of tokens that a sequence does not
+        hold are left as they were (zeros in new tensors)."""
+        import torch
+        S, H = self.num_seqs, self.params.num_kv_heads
+        if not 0 <= n < 1 << 31:
+            raise ValueError(f"n {n}: 0 to 2^31 - 1")
+        starts, first = None, 0
+        if isinstance(start, torch.Tensor):
+            _check_tensor(start, "start", torch.int32, self.device)
+            if start.shape != (S,):
+                raise ValueError(f"start has shape {tuple(start.shape)}, expected {(S,)}")
+            starts = start.data_ptr()
+        else:
+            first = int(start)
+            if not -1 << 31 <= first < 1 << 31:
+                raise ValueError(f"start {first}: a 32-bit integer")
+        shape = (S, H, n, D)
+        k_out, v_out = (torch.zeros(shape, dtype=self.elem, device=self.device) if t is None else t for t in (k_out, v_out))
+        ks, vs = _rows(k_out, "k_out", shape, self.elem, self.device), _rows(v_out, "v_out", shape, self.elem, self.device)
+        if n:
+            _launch(self.device, self._read, self._cp, k_out.data_ptr(), v_out.data_ptr(), _pack3(*ks[:3]), _pack3(*vs[:3]), starts, first, n)
+            self._keep_read = start
+        return k_out, v_out
 
     def _query(self, q, out):
         import torch
@@ -626,8 +646,52 @@ class QuantCache:
     def decode(self, q, sm_scale: float, out=None):
         """Attention over every token: q [S][H * G][128] -> fp32 [S][H * G][128]."""
         out = self._query(q, out)
-        _launch(self.device, self.lib.mosaic_quant_decode_attention, self._cp, q.data_ptr(), out.data_ptr(), float(sm_scale), *self._ws)
+        _launch(self.device, self._decode, self._cp, q.data_ptr(), out.data_ptr(), float(sm_scale), *self._ws)
         return out
+
+
+@dataclass
+class QuantParams:
+    """Shape of an 8-bit cache: codes ("e4m3" or "int8") with one scale for each
+    block of `block` (32 or 64) tokens and kv head."""
+    num_kv_heads: int = 8
+    group_size: int = 4
+    dtype: str = "fp16"
+    format: str = "e4m3"
+    block: int = 32
+
+
+class QuantCache(_BlockCache):
+    """One layer's KV cache in 8 bits for `num_seqs` sequences of up to
+    max_tokens tokens (rounded up to whole blocks).
+
+    The cache is its tensors (attributes; S sequences, H kv heads, N blocks of B
+    tokens): codes k [S][H][N][B][128] and v [S][H][N][128][B], k_scale, v_scale
+    and bound_scale [S][H][N], bounds [S][H][N][2][128], the 16-bit tokens of
+    the unfinished blocks k_tail [S][H][B][128] and v_tail [S][H][128][B], and
+    lens [S][H].  tensors: a dict of these to use in place of new ones (all, or
+    some).  Lengths live on the device: nothing here synchronizes, and captured
+    calls follow them.  Attention takes one query token a sequence, and outputs
+    carry no gradient.  Calls on one cache must be ordered (one stream, or
+    events); they share its workspace."""
+
+    TENSORS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens")
+
+    def __init__(self, params: QuantParams, num_seqs: int, max_tokens: int, device="cuda", tensors=None):
+        import torch
+        given = dict(tensors or {})
+        if params.format not in ("e4m3", "int8"):
+            raise ValueError(f"format {params.format!r}: e4m3 or int8")
+        self._make(params, num_seqs, max_tokens, device, given)
+        S, H, B, N = num_seqs, params.num_kv_heads, params.block, self.max_tokens // params.block
+        code = torch.int8 if params.format == "int8" else torch.float8_e4m3fn
+        shapes = dict(k=((N, B, D), code), v=((N, D, B), code), k_scale=((N,), torch.float32), v_scale=((N,), torch.float32),
+                      bound_scale=((N,), torch.float32), bounds=((N, 2, D), torch.int8), k_tail=((B, D), self.elem),
+                      v_tail=((D, B), self.elem), lens=((), torch.int32))
+        lib = self.lib
+        self._append, self._read, self._decode = lib.mosaic_quant_append, lib.mosaic_quant_read, lib.mosaic_quant_decode_attention
+        self._take(MosaicQuantCache(S, H, params.group_size, D, 1 if params.dtype == "bf16" else 0, 1 if params.format == "int8" else 0, B, N),
+                   shapes, given, lib.mosaic_quant_workspace_bytes)
 
     def decode_selected(self, q, sm_scale: float, select=(1, 10), out=None, blocks=None):
         """Attention over the share select = (num, den) of each (sequence, kv
@@ -644,4 +708,71 @@ class QuantCache:
                 raise ValueError(f"blocks shape {tuple(blocks.shape)} != {tuple(self.k_scale.shape)}")
         _launch(self.device, self.lib.mosaic_quant_select_attention, self._cp, q.data_ptr(), out.data_ptr(), float(sm_scale), int(select[0]),
                 int(select[1]), None if blocks is None else blocks.data_ptr(), *self._ws)
+        return out
+
+
+@dataclass
+class Quant4Params:
+    """Shape of a 4-bit cache: codes with a scale and a zero for each channel's
+    keys of a block of `block` (32 or 64) tokens, and for each token's values."""
+    num_kv_heads: int = 8
+    group_size: int = 4
+    dtype: str = "fp16"
+    block: int = 64
+
+
+class Quant4Cache(_BlockCache):
+    """One layer's KV cache in 4 bits for `num_seqs` sequences of up to
+    max_tokens tokens (rounded up to whole blocks).
+
+    The cache is its tensors (attributes; S sequences, H kv heads, N blocks of B
+    tokens): codes k [S][H][N][B][64] and v [S][H][N][128][B / 2], uint8 of two
+    codes each (of channels, of tokens; the first in the lower half), k_grid
+    [S][H][N][2][128] and v_grid [S][H][N][2][B], scales then zeros of the dtype
+    (a code stands for zero + scale * code), the 16-bit tokens of the unfinished
+    blocks k_tail [S][H][B][128] and v_tail [S][H][128][B], and lens [S][H].
+    tensors: a dict of these to use in place of new ones (all, or some).
+    Lengths live on the device: nothing here synchronizes, and captured calls
+    follow them.  Outputs carry no gradient.  Calls on one cache must be ordered
+    (one stream, or events); they share its workspace."""
+
+    TENSORS = ("k", "v", "k_grid", "v_grid", "k_tail", "v_tail", "lens")
+
+    def __init__(self, params: Quant4Params, num_seqs: int, max_tokens: int, device="cuda", tensors=None):
+        import torch
+        given = dict(tensors or {})
+        self._make(params, num_seqs, max_tokens, device, given)
+        S, H, B, N = num_seqs, params.num_kv_heads, params.block, self.max_tokens // params.block
+        shapes = dict(k=((N, B, D // 2), torch.uint8), v=((N, D, B // 2), torch.uint8), k_grid=((N, 2, D), self.elem),
+                      v_grid=((N, 2, B), self.elem), k_tail=((B, D), self.elem), v_tail=((D, B), self.elem), lens=((), torch.int32))
+        lib = self.lib
+        self._append, self._read, self._decode = lib.mosaic_nibble_append, lib.mosaic_nibble_read, lib.mosaic_nibble_decode_attention
+        self._take(MosaicNibbleCache(S, H, params.group_size, D, 1 if params.dtype == "bf16" else 0, B, N, 0), shapes, given,
+                   lib.mosaic_nibble_workspace_bytes)
+
+    def attend(self, q, sm_scale: float, new_lens=None, causal: bool = True, out=None):
+        """Attention of several query tokens of each sequence: q [S][n][H * G]
+        [128] -> [S][n][H * G][128] of the same type, any strides with contiguous
+        channels.  new_lens: int32 [S] on the GPU, how many of its n queries each
+        sequence has (None: all).  causal: they are its last tokens (in the cache
+        by then), and each attends the tokens up to itself; otherwise each
+        attends every token.  The tokens are those that read() gives.  Rows past
+        new_lens are neither read nor written (zeros in a new tensor)."""
+        import torch
+        S, heads = self.num_seqs, self._q_shape[1]
+        if not isinstance(q, torch.Tensor) or q.dim() != 4:
+            raise ValueError("q must be a tensor [S][n][heads][128]")
+        shape = (S, q.shape[1], heads, D)
+        qs = _rows(q, "q", shape, self.elem, self.device)
+        if new_lens is not None:
+            _check_tensor(new_lens, "new_lens", torch.int32, self.device)
+            if new_lens.shape != (S,):
+                raise ValueError(f"new_lens has shape {tuple(new_lens.shape)}, expected {(S,)}")
+        if out is None:
+            out = (torch.empty if new_lens is None else torch.zeros)(shape, dtype=self.elem, device=self.device)
+        os = _rows(out, "out", shape, self.elem, self.device)
+        if shape[1]:
+            _launch(self.device, self.lib.mosaic_nibble_attend, self._cp, q.data_ptr(), out.data_ptr(), _pack3(*qs[:3]), _pack3(*os[:3]),
+                    None if new_lens is None else new_lens.data_ptr(), shape[1], int(bool(causal)), float(sm_scale), *self._ws)
+            self._keep_attend = (q, new_lens)  # alive until the enqueued work completes
         return out

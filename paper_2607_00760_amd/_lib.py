@@ -20,7 +20,9 @@ EXPORTED = [
     "mosaic_reorder_workspace_bytes", "mosaic_reorder_rotations", "mosaic_decode_attention_noalloc",
     "mosaic_window_poll", "mosaic_window_close", "mosaic_cache_create_ragged", "mosaic_cache_pair_regions",
     "mosaic_window_rotations", "mosaic_qk_norm_rope", "mosaic_quant_append", "mosaic_quant_workspace_bytes",
-    "mosaic_quant_decode_attention", "mosaic_quant_select_attention",
+    "mosaic_quant_decode_attention", "mosaic_quant_select_attention", "mosaic_qk_norm_rope_axes", "mosaic_quant_read",
+    "mosaic_nibble_append", "mosaic_nibble_read", "mosaic_nibble_workspace_bytes", "mosaic_nibble_decode_attention",
+    "mosaic_nibble_attend",
 ]
 
 
@@ -63,6 +65,12 @@ class MosaicQuantCache(C.Structure):
                                          "max_blocks")] + [
         (n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens", "arrivals",
                                   "refused")]
+
+
+class MosaicNibbleCache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("num_seqs", "num_kv_heads", "group_size", "head_dim", "dtype", "block_len", "max_blocks",
+                                         "reserved")] + [
+        (n, C.c_void_p) for n in ("k", "v", "k_grid", "v_grid", "k_tail", "v_tail", "lens", "arrivals", "refused")]
 
 
 class MosaicStats(C.Structure):
@@ -142,6 +150,15 @@ def bind_signatures(L: C.CDLL) -> C.CDLL:
         L.mosaic_quant_workspace_bytes.argtypes = [qc, C.POINTER(sz)]
         L.mosaic_quant_decode_attention.argtypes = [qc, vp, vp, C.c_float, vp, sz, vp]
         L.mosaic_quant_select_attention.argtypes = [qc, vp, vp, C.c_float, C.c_int32, C.c_int32, vp, vp, sz, vp]
+        L.mosaic_quant_read.argtypes = [qc, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, vp]
+    if hasattr(L, "mosaic_nibble_append"):
+        qc = C.POINTER(MosaicNibbleCache)
+        L.mosaic_qk_norm_rope_axes.argtypes = L.mosaic_qk_norm_rope.argtypes[:-1] + [C.c_int32, C.c_char_p, vp]
+        L.mosaic_nibble_append.argtypes = [qc, vp, vp, vp, vp, vp, C.c_int32, vp]
+        L.mosaic_nibble_read.argtypes = [qc, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, vp]
+        L.mosaic_nibble_workspace_bytes.argtypes = [qc, C.POINTER(sz)]
+        L.mosaic_nibble_decode_attention.argtypes = [qc, vp, vp, C.c_float, vp, sz, vp]
+        L.mosaic_nibble_attend.argtypes = [qc, vp, vp, vp, vp, vp, C.c_int32, C.c_int32, C.c_float, vp, sz, vp]
     for n in EXPORTED:
         f = getattr(L, n, None)
         if f is None:

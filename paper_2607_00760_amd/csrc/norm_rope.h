@@ -15,6 +15,9 @@ struct NormRope {
     int64_t pos_seq, pos_tok;
     int seqs, n, hq, hkv, half, pos64, v;
     float eps;
+    int64_t pos_axis;                     // axes: several (positions one pos_axis apart), and each pair's
+    int axes;
+    uint8_t axis[D / 2];
 };
 hipError_t launch_norm_rope(const NormRope &a, int dtype, int interleaved, hipStream_t s);
 

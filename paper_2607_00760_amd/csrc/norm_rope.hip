@@ -15,6 +15,8 @@
 // cosines are made once, and a pair costs six multiplications.  64 lanes
 // compute the token's angles while the rows are on their way.  HBM is the
 // bound: every row is read and written once.
+#include <type_traits>
+
 #include "norm_rope.h"
 
 namespace mosaic {
@@ -59,7 +61,8 @@ template <int DT> __device__ __forceinline__ uint32_t pack(float a, float b) {
 }
 
 // grid (tokens, rounds of a token's rows / rounds of a workgroup, at most NR_AHEAD)
-template <int DT, bool INTER>
+// AXES: pairs turn by the positions of axes of their own.
+template <int DT, bool INTER, bool AXES>
 __global__ void __launch_bounds__(256) k_norm_rope(NormRope a, int rounds) {
     __shared__ __align__(16) float cs[2][D / 2];
     const int tid = threadIdx.x, l = tid & 15, half = a.half;
@@ -95,7 +98,7 @@ __global__ void __launch_bounds__(256) k_norm_rope(NormRope a, int rounds) {
         }
     }
     if (tid < half) {
-        const long long at = s * a.pos_seq + j * a.pos_tok;
+        const long long at = s * a.pos_seq + j * a.pos_tok + (AXES ? a.axis[tid] * a.pos_axis : 0);
         const double pos = a.pos64 ? (double)((const int64_t *)a.pos)[at] : (double)((const int32_t *)a.pos)[at];
         // the angle's turns: the product and 1 / 2 pi in two parts each, so that
         // what is left of positions of 2^50 turns is right to 2^-50
@@ -199,11 +202,13 @@ hipError_t launch_norm_rope(const NormRope &a, int dtype, int interleaved, hipSt
     const int rounds = tokens >= 512 || all > 65535 ? (all < NR_AHEAD ? all : NR_AHEAD) : 1;
     const dim3 grid((uint32_t)tokens, ceil_div(all, rounds));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, rounds); };
-    if (dtype) {
-        if (interleaved) go(k_norm_rope<1, true>); else go(k_norm_rope<1, false>);
-    } else {
-        if (interleaved) go(k_norm_rope<0, true>); else go(k_norm_rope<0, false>);
-    }
+    auto by_axes = [&](auto dt, auto inter) {
+        constexpr int T = decltype(dt)::value;
+        constexpr bool I = decltype(inter)::value;
+        if (a.axes) go(k_norm_rope<T, I, true>); else go(k_norm_rope<T, I, false>);
+    };
+    auto by_order = [&](auto dt) { if (interleaved) by_axes(dt, std::true_type{}); else by_axes(dt, std::false_type{}); };
+    if (dtype) by_order(std::integral_constant<int, 1>{}); else by_order(std::integral_constant<int, 0>{});
     return hipGetLastError();
 }
 

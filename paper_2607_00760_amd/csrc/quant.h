@@ -53,8 +53,8 @@ struct QPlan {
 };
 
 // The plan of run w; units(L): units of a pair of L tokens.
-template <typename U>
-__device__ __forceinline__ QPlan q_plan(const QCache &q, const QShare &sh, U units, int w) {
+template <typename C, typename U>
+__device__ __forceinline__ QPlan q_plan(const C &q, const QShare &sh, U units, int w) {
     const int lane = threadIdx.x & 63;
     auto length = [&](int s) { return s < q.S ? q.len((long long)s * q.H) : 0; };
     const int L0 = length(lane);
