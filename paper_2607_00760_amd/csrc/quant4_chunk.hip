@@ -12,10 +12,11 @@
 // product's rows as the second one asks for them, its weights go into the
 // second product without leaving their lanes.
 //
-// Rows are many or few: with RW = 4 four waves share 64 tokens; with RW = 1
-// each takes 64 tokens of its own and they are joined at the end.  Where there
-// are too few rows for the chip the tokens are split over workgroups, which
-// k_chunk_join joins.
+// Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
+// out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
+// wave takes 64 tokens of its own, keys and values one after the other in LDS of
+// its own, and they are joined at the end.  Where there are too few rows for the
+// chip the tokens are split over workgroups, which k_chunk_join joins.
 #include <type_traits>
 
 #include "quant4.h"
@@ -25,15 +26,20 @@ namespace mosaic {
 namespace {
 
 constexpr int CK_TILE = 64;                                // tokens of a step
-constexpr int CK_WAVES = 4;
-constexpr int CK_SLOTS = 512;                              // workgroups that take part in splits, at most
-constexpr int CK_ROWS = 128;                               // rows of a workgroup at most
+constexpr int CK_SLOTS = 256;                              // workgroups that take part in splits, at most
+constexpr int CK_ROWS = 256;                               // rows of a workgroup at most
+constexpr int CK_FEW = 32, CK_FEW_WAVES = 8;
 
-// Weights are this power of two times as large: as fp16 numbers those of 2^-25
-// and less of the row's largest would vanish, and a million of them count.
-template <int DT> constexpr float CK_POW = DT ? 0.0f : 14.0f;
+// Weights of fp16 are this power of two times as large: those of 2^-25 and less
+// of the row's largest would vanish, and a million of them count.  The running
+// maximum is left behind by up to CK_LAG powers of two, as sums are multiplied
+// through when it moves.
+template <int DT> constexpr float CK_POW = DT ? 0.0f : 10.0f;
+template <int DT> constexpr float CK_LAG = DT ? 8.0f : 4.0f;
 
 typedef __attribute__((ext_vector_type(16))) float cf16;
+typedef __attribute__((ext_vector_type(2))) float cf2;
+typedef __attribute__((ext_vector_type(2))) _Float16 ch2;
 template <int DT> __device__ __forceinline__ cf16 mma32(uint4 a, uint4 b, cf16 c) {
     if constexpr (DT) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(dbf8, a), __builtin_bit_cast(dbf8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(dhf8, a), __builtin_bit_cast(dhf8, b), c, 0, 0, 0);
@@ -46,18 +52,58 @@ template <typename F> __device__ __forceinline__ float halves(float x, F f) {
     return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// zero + scale * code of eight codes, rounded
-template <int DT> __device__ __forceinline__ uint4 values8(uint32_t c, const float (&s)[8], const float (&z)[8]) {
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf(s[i], (float)((c >> (4 * i)) & 15u), z[i]);
-    return make_uint4(pack16<DT>(x[0], x[1]), pack16<DT>(x[2], x[3]), pack16<DT>(x[4], x[5]), pack16<DT>(x[6], x[7]));
+// Eight numbers in the order in which an operand holds them: as they are in
+// bf16; 0, 4, 1, 5, 2, 6, 3, 7 in fp16, as two codes come out of one mask.
+template <int DT> __device__ __forceinline__ uint4 dealt(uint4 w) {
+    if constexpr (DT) return w;
+    return make_uint4(__builtin_amdgcn_perm(w.z, w.x, 0x05040100u), __builtin_amdgcn_perm(w.z, w.x, 0x07060302u),
+                      __builtin_amdgcn_perm(w.w, w.y, 0x05040100u), __builtin_amdgcn_perm(w.w, w.y, 0x07060302u));
 }
-template <int DT> __device__ __forceinline__ void widen8(uint4 w, float (&x)[8]) {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+template <int DT> __device__ __forceinline__ constexpr int deal(int i) { return DT ? i : (i >> 1) + 4 * (i & 1); }
+
+// Grids of eight codes, ready for values(): fp32 numbers, or dealt fp16 pairs
+template <int DT> struct Grid8;
+template <> struct Grid8<1> {
+    float s[8], z[8];
+    __device__ __forceinline__ Grid8(uint4 sw, uint4 zw) {
+        const uint32_t a[4] = {sw.x, sw.y, sw.z, sw.w}, b[4] = {zw.x, zw.y, zw.z, zw.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = half_of<DT>(u, i);
-}
+        for (int i = 0; i < 8; ++i) { s[i] = half_of<1>(a, i); z[i] = half_of<1>(b, i); }
+    }
+    // zero + scale * code, rounded (a code is, as an E4M3 byte, itself times 2^-9)
+    __device__ __forceinline__ uint4 values(uint32_t c) const {
+        const uint32_t lo = c & 0x0f0f0f0fu, hi = (c >> 4) & 0x0f0f0f0fu;
+        const cf2 e0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, 512.0f, false), e1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(lo, 512.0f, true);
+        const cf2 o0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, 512.0f, false), o1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi, 512.0f, true);
+        return make_uint4(pack16<1>(fmaf(s[0], e0[0], z[0]), fmaf(s[1], o0[0], z[1])), pack16<1>(fmaf(s[2], e0[1], z[2]), fmaf(s[3], o0[1], z[3])),
+                          pack16<1>(fmaf(s[4], e1[0], z[4]), fmaf(s[5], o1[0], z[5])), pack16<1>(fmaf(s[6], e1[1], z[6]), fmaf(s[7], o1[1], z[7])));
+    }
+};
+template <> struct Grid8<0> {
+    ch2 s[4], z[4];
+    __device__ __forceinline__ Grid8(uint4 sw, uint4 zw) {
+        sw = dealt<0>(sw);
+        zw = dealt<0>(zw);
+        __builtin_memcpy(s, &sw, 16);
+        __builtin_memcpy(z, &zw, 16);
+    }
+    // the same in fp16, one rounding (a code's bits under 1024 are 1024 + code)
+    __device__ __forceinline__ uint4 values(uint32_t c) const {
+        const ch2 off = {(_Float16)1024.0f, (_Float16)1024.0f}, by = {(_Float16)0.0625f, (_Float16)0.0625f}, off16 = {(_Float16)-64.0f, (_Float16)-64.0f};
+        ch2 o[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t u = e ? c >> 8 : c;
+            const ch2 a = __builtin_bit_cast(ch2, (u & 0x000f000fu) | 0x64006400u) - off;
+            const ch2 b = __builtin_elementwise_fma(__builtin_bit_cast(ch2, (u & 0x00f000f0u) | 0x64006400u), by, off16);
+            o[2 * e] = __builtin_elementwise_fma(s[2 * e], a, z[2 * e]);
+            o[2 * e + 1] = __builtin_elementwise_fma(s[2 * e + 1], b, z[2 * e + 1]);
+        }
+        uint4 r;
+        __builtin_memcpy(&r, o, 16);
+        return r;
+    }
+};
 
 // a row tile's share of the work, the same in the attention and in the join
 struct ChunkPlan {
@@ -81,133 +127,143 @@ __device__ __forceinline__ ChunkPlan chunk_plan(const Q4Cache &q, const QChunk &
     return r;
 }
 
-template <int B, int DT, int RW>
-__global__ void __launch_bounds__(64 * CK_WAVES)
-k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
-    constexpr int TW = CK_WAVES / RW, GT = 64 * RW;        // groups of waves with a step of their own, threads of a group
-    constexpr int KR = GT / 16, KP = CK_TILE / KR;         // keys: tokens of a pass, passes
-    constexpr int VR = GT / 8, VP = D / VR;                // values: channels of a pass, passes
-    constexpr int NB = CK_TILE / B;                        // blocks of a step
-    __shared__ __align__(16) uint8_t lds[TW][2 * CK_TILE * D * 2];
-    __shared__ float ml[CK_WAVES][32][2];
-    const int id = blockIdx.x / ns, split = blockIdx.x - id * ns;
-    const ChunkPlan pl = chunk_plan(q, c, id, tiles, 32 * RW, ns);
-    if (pl.row0 >= pl.m * q.G) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tw = wave / RW, rw = wave % RW, gt = tid & (GT - 1);
-    const int t0 = split * pl.per, t1 = min(pl.nt, t0 + pl.per);
-    if (split > 0 && t0 >= t1) return;                     // (split 0 writes what nothing is seen of, too)
-    uint8_t *kl = lds[tw], *vl = lds[tw] + CK_TILE * D * 2;
-    const int l32 = lane & 31, hl = lane >> 5;
-    const int row = pl.row0 + 32 * rw + l32, qi = row / q.G, head = pl.h * q.G + row - qi * q.G;
-    const bool valid = qi < pl.m;
-    const int seen = valid ? (c.causal ? pl.L - pl.m + qi + 1 : pl.L) : 0;     // tokens that the row attends
-    const int all = c.causal ? pl.L - pl.m + pl.row0 / q.G + 1 : pl.L;         // that every row of the workgroup does
-    const float zs = fabsf(c.scale) * 1.44269504088896340736f;
-    uint4 qf[8];                                           // channels 16 e + 8 hl + [0, 8) of the row
-    {
-        const uint16_t *qp = c.q + pl.s * c.q_seq + qi * c.q_tok + head * c.q_head + 8 * hl;
-        const uint32_t flip = c.scale < 0.0f ? 0x80008000u : 0u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            qf[e] = valid ? *(const uint4 *)(qp + 16 * e) : make_uint4(0, 0, 0, 0);
-            qf[e].x ^= flip; qf[e].y ^= flip; qf[e].z ^= flip; qf[e].w ^= flip;
-        }
-    }
-    // keys: tokens kt0 + KR i, channels 8 kc + [0, 8); values: channels vc0 + VR i, tokens 8 vo + [0, 8)
-    const int kt0 = gt >> 4, kc = gt & 15, vc0 = gt >> 3, vo = gt & 7;
-    const int whole = pl.L / B, tail = pl.L % B;
-    const uint64_t pb = (uint64_t)pl.p * q.N;
+// A step's 64 tokens worked out by GT threads (thread gt): keys at kl by token,
+// rows of 256 bytes, values at vl by channel, rows of 128, both with the 16-byte
+// pieces of a row turned so that the operands' reads spread over the banks.
+template <int B, int DT, int GT> struct Step {
+    static constexpr int KR = GT / 16, KP = CK_TILE / KR;  // keys: tokens of a pass, passes
+    static constexpr int VR = GT / 8, VP = D / VR;         // values: channels of a pass, passes
+    static constexpr int NB = CK_TILE / B;                 // blocks of a step
     uint32_t kq[KP], vq[VP];
     uint4 kg[NB][2], vg[2];
-    auto load = [&](int t) {                               // the step's codes and grids (blocks that are whole)
+    static __device__ __forceinline__ uint4 *k_at(uint8_t *kl, int t, int piece) { return (uint4 *)(kl + t * 256 + 16 * (piece ^ (t & 15))); }
+    static __device__ __forceinline__ uint4 *v_at(uint8_t *vl, int ch, int piece) { return (uint4 *)(vl + ch * 128 + 16 * (piece ^ ((ch >> 1) & 7))); }
+    // codes and grids of step t, if its blocks are whole
+    __device__ __forceinline__ void load_k(const Q4Cache &q, uint64_t pb, int whole, int t, int gt) {
+        if (NB * (t + 1) > whole) return;
+        const uint64_t blk = pb + (uint32_t)(NB * t);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            if (NB * t + b >= whole) continue;
-            const uint64_t blk = pb + (uint32_t)(NB * t + b);
-            const uint16_t *g = q.kg + blk * (2 * D) + 8 * kc;
+            const uint16_t *g = q.kg + (blk + b) * (2 * D) + 8 * (gt & 15);
             kg[b][0] = *(const uint4 *)g;
             kg[b][1] = *(const uint4 *)(g + D);
         }
+        // (blocks lie one after the other, and so do their tokens)
+        const uint8_t *kp = q.k + blk * (B * D / 2) + 4 * gt;
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            const int tk = kt0 + KR * i, b = NB * t + tk / B;
-            if (b < whole) kq[i] = *(const uint32_t *)(q.k + (pb + (uint32_t)b) * (B * D / 2) + (tk % B) * (D / 2) + 4 * kc);
-        }
-        const int b = NB * t + 8 * vo / B, at = 8 * vo % B;
-        if (b < whole) {
-            const uint64_t blk = pb + (uint32_t)b;
-            vg[0] = *(const uint4 *)(q.vg + blk * (2 * B) + at);
-            vg[1] = *(const uint4 *)(q.vg + blk * (2 * B) + B + at);
+        for (int i = 0; i < KP; ++i) kq[i] = *(const uint32_t *)(kp + 4 * GT * i);
+    }
+    __device__ __forceinline__ void load_v(const Q4Cache &q, uint64_t pb, int whole, int t, int gt) {
+        if (NB * (t + 1) > whole) return;
+        const int vo = gt & 7, at = 8 * vo % B;
+        const uint64_t blk = pb + (uint32_t)(NB * t + 8 * vo / B);
+        vg[0] = *(const uint4 *)(q.vg + blk * (2 * B) + at);
+        vg[1] = *(const uint4 *)(q.vg + blk * (2 * B) + B + at);
+        const uint8_t *vp = q.v + blk * (B * D / 2) + (gt >> 3) * (B / 2) + at / 2;
 #pragma unroll
-            for (int i = 0; i < VP; ++i) vq[i] = *(const uint32_t *)(q.v + blk * (B * D / 2) + (vc0 + VR * i) * (B / 2) + at / 2);
-        }
-    };
-    auto k_at = [&](int t, int piece) { return (uint4 *)(kl + t * 256 + 16 * (piece ^ (t & 15))); };
-    auto v_at = [&](int ch, int piece) { return (uint4 *)(vl + ch * 128 + 16 * (piece ^ ((ch >> 1) & 7))); };
-    auto store = [&](int t) {                              // into LDS; tokens past the last are zeros
+        for (int i = 0; i < VP; ++i) vq[i] = *(const uint32_t *)(vp + VR * (B / 2) * i);
+    }
+    // into LDS; the last step, with tokens of no whole block, is read here one
+    // pass after the other, and tokens past the last are zeros
+    __device__ __forceinline__ void store_k(const Q4Cache &q, int p, uint64_t pb, int whole, int tail, int t, int gt, uint8_t *kl) const {
+        const int kc = gt & 15;
+        if (NB * (t + 1) <= whole) {
 #pragma unroll
-        for (int i = 0; i < KP; ++i) {
-            const int tk = kt0 + KR * i, bi = tk / B, b = NB * t + bi;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (b < whole) {
-                float s[8], z[8];
-                widen8<DT>(kg[bi][0], s);
-                widen8<DT>(kg[bi][1], z);
-                x = values8<DT>(kq[i], s, z);
-            } else if (b == whole && tk % B < tail) {
-                x = *(const uint4 *)(q.kt + ((uint64_t)pl.p * B + tk % B) * D + 8 * kc);
+            for (int b = 0; b < NB; ++b) {
+                const Grid8<DT> g(kg[b][0], kg[b][1]);
+#pragma unroll
+                for (int i = b * (KP / NB); i < (b + 1) * (KP / NB); ++i) *k_at(kl, (gt >> 4) + KR * i, kc) = g.values(kq[i]);
             }
-            *k_at(tk, kc) = x;
+            return;
         }
-        const int b = NB * t + 8 * vo / B, at = 8 * vo % B;
-        float s[8], z[8];
-        widen8<DT>(vg[0], s);
-        widen8<DT>(vg[1], z);
-#pragma unroll
-        for (int i = 0; i < VP; ++i) {
-            const int ch = vc0 + VR * i;
+#pragma unroll 1
+        for (int tk = gt >> 4; tk < CK_TILE; tk += KR) {
+            const int b = NB * t + tk / B;
             uint4 x = make_uint4(0, 0, 0, 0);
             if (b < whole) {
-                x = values8<DT>(vq[i], s, z);
+                const uint64_t blk = pb + (uint32_t)b;
+                const uint16_t *g = q.kg + blk * (2 * D) + 8 * kc;
+                x = Grid8<DT>(*(const uint4 *)g, *(const uint4 *)(g + D)).values(*(const uint32_t *)(q.k + blk * (B * D / 2) + (tk % B) * (D / 2) + 4 * kc));
+            } else if (b == whole && tk % B < tail) {
+                x = dealt<DT>(*(const uint4 *)(q.kt + ((uint64_t)p * B + tk % B) * D + 8 * kc));
+            }
+            *k_at(kl, tk, kc) = x;
+        }
+    }
+    __device__ __forceinline__ void store_v(const Q4Cache &q, int p, uint64_t pb, int whole, int tail, int t, int gt, uint8_t *vl) const {
+        const int vo = gt & 7, b = NB * t + 8 * vo / B, at = 8 * vo % B;
+        if (NB * (t + 1) <= whole) {
+            const Grid8<DT> g(vg[0], vg[1]);
+#pragma unroll
+            for (int i = 0; i < VP; ++i) *v_at(vl, (gt >> 3) + VR * i, vo) = g.values(vq[i]);
+            return;
+        }
+#pragma unroll 1
+        for (int ch = gt >> 3; ch < D; ch += VR) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (b < whole) {
+                const uint64_t blk = pb + (uint32_t)b;
+                const uint16_t *g = q.vg + blk * (2 * B) + at;
+                x = Grid8<DT>(*(const uint4 *)g, *(const uint4 *)(g + B)).values(*(const uint32_t *)(q.v + blk * (B * D / 2) + ch * (B / 2) + at / 2));
             } else if (b == whole) {
                 const int keep = tail - at;                // tokens of the eight
-                if (keep > 0) x = *(const uint4 *)(q.vt + ((uint64_t)pl.p * D + ch) * B + at);
+                if (keep > 0) x = *(const uint4 *)(q.vt + ((uint64_t)p * D + ch) * B + at);
                 x.x = keep >= 2 ? x.x : (keep == 1 ? x.x & 0xffffu : 0u);
                 x.y = keep >= 4 ? x.y : (keep == 3 ? x.y & 0xffffu : 0u);
                 x.z = keep >= 6 ? x.z : (keep == 5 ? x.z & 0xffffu : 0u);
                 x.w = keep >= 8 ? x.w : (keep == 7 ? x.w & 0xffffu : 0u);
+                x = dealt<DT>(x);
             }
-            *v_at(ch, vo) = x;
+            *v_at(vl, ch, vo) = x;
         }
-    };
-    cf16 acc[4];                                           // [32 channels][8 (i / 4) + 4 hl + i % 4], the lane's row
+    }
+};
+
+// A wave's 32 rows: lanes l and l + 32 share row l % 32
+template <int DT> struct Rows {
+    uint4 qf[8];                                           // channels 16 e + 8 hl + [0, 8)
+    cf16 acc[4];                                           // channel 32 ct + 8 (i / 4) + 4 hl + i % 4
+    float m_run, l_run, mz, zs;                            // maximum, the lane's sum; what logits are lessened by, and scaled
+    int seen;                                              // tokens that the row attends
+    bool valid;
+    __device__ __forceinline__ void begin(const Q4Cache &q, const QChunk &c, const ChunkPlan &pl, int row, int hl) {
+        const int qi = row / q.G, head = pl.h * q.G + row - qi * q.G;
+        valid = qi < pl.m;
+        seen = valid ? (c.causal ? pl.L - pl.m + qi + 1 : pl.L) : 0;
+        zs = fmaxf(fabsf(c.scale) * 1.44269504088896340736f, 0x1p-120f);  // (0: every logit's power is 1; a masked one's is not)
+        const uint16_t *qp = c.q + pl.s * c.q_seq + qi * c.q_tok + head * c.q_head + 8 * hl;
+        const uint32_t flip = c.scale < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int ct = 0; ct < 4; ++ct)
+        for (int e = 0; e < 8; ++e) {
+            const uint4 w = valid ? *(const uint4 *)(qp + 16 * e) : make_uint4(0, 0, 0, 0);
+            qf[e] = dealt<DT>(make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip));
+        }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
-    float m_run = -INFINITY, l_run = 0.0f;
-    // row r of the first product is the step's token (r & 16) + 8 (r / 4 & 1) + 4 (r / 8 & 1) + r % 4
-    const int tau = (l32 & 16) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
-    const int turns = (t1 - t0 + TW - 1) / TW;
-    if (t0 + tw < t1) load(t0 + tw);
-    for (int u = 0; u < turns; ++u) {
-        const int t = t0 + u * TW + tw;
-        lds_barrier();                                     // the last step has been read
-        if (t < t1) store(t);
-        if (t + TW < t1) load(t + TW);
-        lds_barrier();
-        if (t >= t1) continue;
-        cf16 z[2];
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[ct][i] = 0.0f;
+        m_run = -INFINITY;
+        l_run = 0.0f;
+        mz = CK_POW<DT>;
+    }
+    // logits of the 64 tokens at kl: z[n][i] of token 32 n + 16 (i / 8) + 8 hl + i % 8.  (Row r of the product is token
+    // (r & 16) + 8 (r / 4 & 1) + 4 (r / 8 & 1) + r % 4.)
+    __device__ __forceinline__ void logits(uint8_t *kl, int lane, cf16 (&z)[2]) const {
+        const int l32 = lane & 31, hl = lane >> 5;
+        const int tau = (l32 & 16) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
+        const uint8_t *row = kl + tau * 256;
+        const int at = 16 * (hl ^ (tau & 15));
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[n][i] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[n] = mma32<DT>(*k_at(32 * n + tau, 2 * e + hl), qf[e], z[n]);
+            for (int e = 0; e < 8; ++e) z[n] = mma32<DT>(*(const uint4 *)(row + (at ^ (32 * e)) + 8192 * n), qf[e], z[n]);
         }
-        // z[n][i]: token 64 t + 32 n + 16 (i / 8) + 8 hl + i % 8
-        if (CK_TILE * (t + 1) > all) {                     // some row does not see all of them
+    }
+    // the softmax's step: weights of tokens 16 e + 8 hl + [0, 8), dealt
+    __device__ __forceinline__ void weigh(cf16 (&z)[2], int t, int hl, bool masked, uint4 (&pf)[4]) {
+        if (masked) {
             const int left = seen - (CK_TILE * t + 8 * hl);
 #pragma unroll
             for (int n = 0; n < 2; ++n)
@@ -221,83 +277,185 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) cm = fmaxf(cm, z[n][i]);
         cm = halves(cm, [](float a, float b) { return fmaxf(a, b); });
-        const float mn = fmaxf(m_run, cm), mb = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - mb) * zs);
-        m_run = mn;
-        l_run *= alpha;
-        uint4 pf[4];                                       // weights of tokens 16 e + 8 hl + [0, 8)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = z[e >> 1][8 * (e & 1) + i];
-                x[i] = d == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(d - mb, zs, CK_POW<DT>));
-                l_run += x[i];
-            }
-            pf[e] = make_uint4(pack16<DT>(x[0], x[1]), pack16<DT>(x[2], x[3]), pack16<DT>(x[4], x[5]), pack16<DT>(x[6], x[7]));
-        }
-        if (!__all(alpha == 1.0f)) {
+        if (__any((cm - m_run) * zs > CK_LAG<DT>)) {
+            const float mn = fmaxf(m_run, cm), mb = mn == -INFINITY ? 0.0f : mn;
+            const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m_run - mb) * zs);
+            m_run = mn;
+            mz = CK_POW<DT> - mb * zs;
+            l_run *= alpha;
 #pragma unroll
             for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[ct][i] *= alpha;
         }
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
+        for (int e = 0; e < 4; ++e) {
+            float x[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[ct] = mma32<DT>(*v_at(32 * ct + l32, 2 * e + hl), pf[e], acc[ct]);
-    }
-    l_run = halves(l_run, [](float a, float b) { return a + b; });
-    if (TW > 1) {                                          // the waves joined, each a quarter of the channels
-        __syncthreads();
-        float *mine = (float *)lds[0];                     // [wave][channel][row]: 64 KB of 128
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mine[(wave * D + 32 * ct + 8 * (i >> 2) + 4 * hl + (i & 3)) * 32 + l32] = acc[ct][i];
-        if (hl == 0) { ml[wave][l32][0] = m_run; ml[wave][l32][1] = l_run; }
-        __syncthreads();
-        float m[CK_WAVES], f[CK_WAVES];
-        m_run = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < CK_WAVES; ++w) { m[w] = ml[w][l32][0]; m_run = fmaxf(m_run, m[w]); }
-        l_run = 0.0f;
-#pragma unroll
-        for (int w = 0; w < CK_WAVES; ++w) {
-            f[w] = m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[w] - m_run) * zs);
-            l_run += f[w] * ml[w][l32][1];
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {                     // channels 32 wave + 8 (i / 4) + 4 hl + i % 4
-            float a = 0.0f;
-#pragma unroll
-            for (int w = 0; w < CK_WAVES; ++w) a += f[w] * mine[(w * D + 32 * wave + 8 * (i >> 2) + 4 * hl + (i & 3)) * 32 + l32];
-            acc[0][i] = a;
+            for (int i = 0; i < 8; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(z[e >> 1][8 * (e & 1) + i], zs, mz));
+                l_run += x[i];
+            }
+            pf[e] = make_uint4(pack16<DT>(x[deal<DT>(0)], x[deal<DT>(1)]), pack16<DT>(x[deal<DT>(2)], x[deal<DT>(3)]),
+                               pack16<DT>(x[deal<DT>(4)], x[deal<DT>(5)]), pack16<DT>(x[deal<DT>(6)], x[deal<DT>(7)]));
         }
     }
-    const float inv = l_run > 0.0f ? 1.0f / l_run : (l_run != l_run ? l_run : 0.0f);
-    const int ch0 = TW > 1 ? 32 * wave : 0;
+    __device__ __forceinline__ void add(uint8_t *vl, int lane, const uint4 (&pf)[4]) {
+        const int l32 = lane & 31, hl = lane >> 5;
+        const uint8_t *row = vl + l32 * 128;
+        const int at = 16 * (hl ^ ((l32 >> 1) & 7));
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[ct] = mma32<DT>(*(const uint4 *)(row + (at ^ (32 * e)) + 4096 * ct), pf[e], acc[ct]);
+    }
+};
+
+__device__ __forceinline__ float share_of(float s) { return s > 0.0f ? 1.0f / s : (s != s ? s : 0.0f); }
+__device__ __forceinline__ uint16_t *out_row(const Q4Cache &q, const QChunk &c, const ChunkPlan &pl, int row) {
+    const int qi = row / q.G, head = pl.h * q.G + row - qi * q.G;
+    return c.out + pl.s * c.o_seq + qi * c.o_tok + head * c.o_head;
+}
+__device__ __forceinline__ float power_of(float m, float zs) { return m == -INFINITY ? m : m * zs; }
+
+// grid (row tiles, splits and pairs); RW waves of 32 rows
+template <int B, int DT, int RW>
+__global__ void __launch_bounds__(64 * RW) __attribute__((amdgpu_waves_per_eu(2)))
+k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
+    constexpr int KB = CK_TILE * D * 2;                    // bytes of a step's keys, and of its values
+    __shared__ __align__(16) uint8_t lds[2][2 * KB];
+    const int id = blockIdx.x / ns, split = blockIdx.x - id * ns;
+    const ChunkPlan pl = chunk_plan(q, c, id, tiles, 32 * RW, ns);
+    if (pl.row0 >= pl.m * q.G) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t0 = split * pl.per, t1 = min(pl.nt, t0 + pl.per);
+    if (split > 0 && t0 >= t1) return;                     // (split 0 writes what nothing is seen of, too)
+    const int hl = lane >> 5, row = pl.row0 + 32 * wave + (lane & 31);
+    const int all = c.causal ? pl.L - pl.m + pl.row0 / q.G + 1 : pl.L;     // tokens that every row of the workgroup attends
+    const int whole = pl.L / B, tail = pl.L % B;
+    const uint64_t pb = (uint64_t)pl.p * q.N;
+    Step<B, DT, 64 * RW> st;
+    auto load = [&](int t) { st.load_k(q, pb, whole, t, tid); st.load_v(q, pb, whole, t, tid); };
+    auto store = [&](int t, int b) { st.store_k(q, pl.p, pb, whole, tail, t, tid, lds[b]); st.store_v(q, pl.p, pb, whole, tail, t, tid, lds[b] + KB); };
+    Rows<DT> r;
+    if (t0 < t1) load(t0);
+    r.begin(q, c, pl, row, hl);
+    if (t0 < t1) store(t0, 0);
+    if (t0 + 1 < t1) load(t0 + 1);
+    for (int t = t0; t < t1; ++t) {
+        const int b = (t - t0) & 1;
+        lds_barrier();                                     // this step's are there, the last one's have been read
+        cf16 z[2];
+        uint4 pf[4];
+        r.logits(lds[b], lane, z);
+        if (t + 1 < t1) {
+            store(t + 1, b ^ 1);
+            if (t + 2 < t1) load(t + 2);
+        }
+        r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
+        r.add(lds[b] + KB, lane, pf);
+    }
+    const float l = halves(r.l_run, [](float a, float b) { return a + b; }), inv = share_of(l);
     if (pl.used <= 1) {
-        if (!valid) return;
-        uint16_t *op = c.out + pl.s * c.o_seq + qi * c.o_tok + head * c.o_head + ch0 + 4 * hl;
+        if (!r.valid) return;
+        uint16_t *op = out_row(q, c, pl, row) + 4 * hl;
 #pragma unroll
-        for (int ct = 0; ct < (TW > 1 ? 1 : 4); ++ct)
+        for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
             for (int a = 0; a < 4; ++a)
-                *(uint2 *)(op + 32 * ct + 8 * a) = make_uint2(pack16<DT>(acc[ct][4 * a] * inv, acc[ct][4 * a + 1] * inv),
-                                                              pack16<DT>(acc[ct][4 * a + 2] * inv, acc[ct][4 * a + 3] * inv));
+                *(uint2 *)(op + 32 * ct + 8 * a) = make_uint2(pack16<DT>(r.acc[ct][4 * a] * inv, r.acc[ct][4 * a + 1] * inv),
+                                                              pack16<DT>(r.acc[ct][4 * a + 2] * inv, r.acc[ct][4 * a + 3] * inv));
         return;
     }
     // a split's averages, and (maximum, sum)
-    float *to = part + (uint64_t)blockIdx.x * (32 * RW) * (D + 4) + (row - pl.row0) * (D + 4);
-    if (hl == 0 && (TW == 1 || wave == 0)) *(float2 *)to = make_float2(m_run == -INFINITY ? m_run : m_run * zs, l_run);
+    float *to = part + ((uint64_t)blockIdx.x * (32 * RW) + (row - pl.row0)) * (D + 4);
+    if (hl == 0) *(float2 *)to = make_float2(power_of(r.m_run, r.zs), l);
 #pragma unroll
-    for (int ct = 0; ct < (TW > 1 ? 1 : 4); ++ct)
+    for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
         for (int a = 0; a < 4; ++a)
-            *(float4 *)(to + 4 + ch0 + 32 * ct + 8 * a + 4 * hl) = make_float4(acc[ct][4 * a] * inv, acc[ct][4 * a + 1] * inv, acc[ct][4 * a + 2] * inv,
-                                                                               acc[ct][4 * a + 3] * inv);
+            *(float4 *)(to + 4 + 32 * ct + 8 * a + 4 * hl) = make_float4(r.acc[ct][4 * a] * inv, r.acc[ct][4 * a + 1] * inv,
+                                                                         r.acc[ct][4 * a + 2] * inv, r.acc[ct][4 * a + 3] * inv);
+}
+
+// at most 32 rows: grid (splits and pairs)
+template <int B, int DT>
+__global__ void __launch_bounds__(64 * CK_FEW_WAVES) __attribute__((amdgpu_waves_per_eu(2)))
+k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
+    constexpr int W = CK_FEW_WAVES, KB = CK_TILE * D * 2;
+    __shared__ __align__(16) uint8_t lds[W][KB];
+    __shared__ float ml[W][32][2];
+    const int id = blockIdx.x / ns, split = blockIdx.x - id * ns;
+    const ChunkPlan pl = chunk_plan(q, c, id, 1, CK_FEW, ns);
+    if (pl.m == 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t0 = split * pl.per, t1 = min(pl.nt, t0 + pl.per);
+    if (split > 0 && t0 >= t1) return;                     // (split 0 writes what nothing is seen of, too)
+    const int l32 = lane & 31, hl = lane >> 5;
+    const int all = c.causal ? pl.L - pl.m + 1 : pl.L;     // tokens that every row attends
+    const int whole = pl.L / B, tail = pl.L % B;
+    const uint64_t pb = (uint64_t)pl.p * q.N;
+    uint8_t *mine = lds[wave];
+    Step<B, DT, 64> st;
+    int t = t0 + wave;
+    if (t < t1) { st.load_k(q, pb, whole, t, lane); st.load_v(q, pb, whole, t, lane); }
+    Rows<DT> r;
+    r.begin(q, c, pl, l32, hl);
+    for (; t < t1; t += W) {
+        cf16 z[2];
+        uint4 pf[4];
+        st.store_k(q, pl.p, pb, whole, tail, t, lane, mine);
+        mem_fence_compiler();
+        wave_sync();
+        if (t + W < t1) st.load_k(q, pb, whole, t + W, lane);
+        r.logits(mine, lane, z);
+        mem_fence_compiler();
+        wave_sync();
+        st.store_v(q, pl.p, pb, whole, tail, t, lane, mine);   // (the wave's LDS operations run in their order)
+        mem_fence_compiler();
+        wave_sync();
+        if (t + W < t1) st.load_v(q, pb, whole, t + W, lane);
+        r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
+        r.add(mine, lane, pf);
+        mem_fence_compiler();
+        wave_sync();
+    }
+    // the waves joined, in their order; each takes 16 channels
+    float l = halves(r.l_run, [](float a, float b) { return a + b; });
+    float *sums = (float *)mine;                           // [channel][row]
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[(32 * ct + 8 * (i >> 2) + 4 * hl + (i & 3)) * 32 + l32] = r.acc[ct][i];
+    if (hl == 0) { ml[wave][l32][0] = r.m_run; ml[wave][l32][1] = l; }
+    __syncthreads();
+    float m = -INFINITY, f[W], x[8];
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, ml[w][l32][0]);
+    l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        f[w] = ml[w][l32][0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ml[w][l32][0] - m) * r.zs);
+        l += f[w] * ml[w][l32][1];
+    }
+    const float inv = share_of(l);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {                          // channels 16 wave + 8 hl + i
+        x[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) x[i] += f[w] * ((const float *)lds[w])[(16 * wave + 8 * hl + i) * 32 + l32];
+        x[i] *= inv;
+    }
+    if (pl.used <= 1) {
+        if (r.valid)
+            *(uint4 *)(out_row(q, c, pl, l32) + 16 * wave + 8 * hl) = make_uint4(pack16<DT>(x[0], x[1]), pack16<DT>(x[2], x[3]), pack16<DT>(x[4], x[5]),
+                                                                                 pack16<DT>(x[6], x[7]));
+        return;
+    }
+    float *to = part + ((uint64_t)blockIdx.x * CK_FEW + l32) * (D + 4);
+    if (wave == 0 && hl == 0) *(float2 *)to = make_float2(power_of(m, r.zs), l);
+    *(float4 *)(to + 4 + 16 * wave + 8 * hl) = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4 *)(to + 8 + 16 * wave + 8 * hl) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
 // the splits of a row tile joined, in their order; grid (row tiles and pairs, rows / 8), 32 lanes a row
@@ -318,7 +476,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(Q4Cache q, QChunk c, int til
         const float mn = fmaxf(M, x.x), mb = mn == -INFINITY ? 0.0f : mn;
         float f = S * __builtin_amdgcn_exp2f(M - mb), g = x.y * __builtin_amdgcn_exp2f(x.x - mb);
         S = f + g;
-        const float inv = S > 0.0f ? 1.0f / S : (S != S ? S : 0.0f);
+        const float inv = share_of(S);
         f *= inv;
         g *= inv;
         A = make_float4(A.x * f + a.x * g, A.y * f + a.y * g, A.z * f + a.z * g, A.w * f + a.w * g);
@@ -333,16 +491,18 @@ size_t quant4_chunk_ws_bytes() { return (size_t)CK_SLOTS * CK_ROWS * (D + 4) * s
 
 hipError_t launch_quant4_chunk(const Q4Cache &q, int block, int dtype, const QChunk &c, float *part, hipStream_t s) {
     const int pairs = q.S * q.H, all = c.n * q.G;
-    const int rows = all <= 32 ? 32 : CK_ROWS, tiles = (all + rows - 1) / rows;
+    const int rows = all <= CK_FEW ? CK_FEW : (all <= 128 ? 128 : CK_ROWS), tiles = (all + rows - 1) / rows;
     const long long wgs = (long long)pairs * tiles;
-    const int most = ceil_div(q.cap, 4 * CK_TILE);         // (four steps a split at least)
+    // a split has a step for each wave (of few rows) or four at least
+    const int most = ceil_div(q.cap, (rows == CK_FEW ? CK_FEW_WAVES : 4) * CK_TILE);
     int ns = (int)(CK_SLOTS / wgs);
     ns = ns < 1 ? 1 : (ns > most ? most : ns);
     const dim3 grid((uint32_t)(wgs * ns));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * CK_WAVES), 0, s, q, c, tiles, ns, part); };
     auto by_rows = [&](auto b, auto dt) {
         constexpr int BL = decltype(b)::value, T = decltype(dt)::value;
-        if (rows == 32) go(k_chunk<BL, T, 1>); else go(k_chunk<BL, T, 4>);
+        if (rows == CK_FEW) hipLaunchKernelGGL((k_chunk_few<BL, T>), grid, dim3(64 * CK_FEW_WAVES), 0, s, q, c, ns, part);
+        else if (rows == 128) hipLaunchKernelGGL((k_chunk<BL, T, 4>), grid, dim3(256), 0, s, q, c, tiles, ns, part);
+        else hipLaunchKernelGGL((k_chunk<BL, T, 8>), grid, dim3(512), 0, s, q, c, tiles, ns, part);
     };
     auto by_type = [&](auto b) { if (dtype) by_rows(b, std::integral_constant<int, 1>{}); else by_rows(b, std::integral_constant<int, 0>{}); };
     if (block == 32) by_type(std::integral_constant<int, 32>{}); else by_type(std::integral_constant<int, 64>{});
