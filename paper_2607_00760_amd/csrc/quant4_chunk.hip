@@ -12,8 +12,11 @@
 // product's rows as the second one asks for them, its weights go into the
 // second product without leaving their lanes.
 //
-// Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
-// out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
+// Rows are many or few.  Many: all waves of a workgroup share 64 tokens.  A
+// wave's step is a turn on the matrix cores (O of step i, S of step i + 1) and
+// one on the vector ALU (the softmax of step i + 1, its part of later steps
+// worked out into LDS); of the two waves on a SIMD one takes the first kind of
+// turn while the other takes the second.  At most 32 (k_chunk_few): each
 // wave takes 64 tokens of its own, keys and values one after the other in LDS of
 // its own, and they are joined at the end.  Where there are too few rows for the
 // chip the tokens are split over workgroups, which k_chunk_join joins.
@@ -246,19 +249,47 @@ template <int DT> struct Rows {
         l_run = 0.0f;
         mz = CK_POW<DT>;
     }
-    // logits of the 64 tokens at kl: z[n][i] of token 32 n + 16 (i / 8) + 8 hl + i % 8.  (Row r of the product is token
-    // (r & 16) + 8 (r / 4 & 1) + 4 (r / 8 & 1) + r % 4.)
-    __device__ __forceinline__ void logits(uint8_t *kl, int lane, cf16 (&z)[2]) const {
+    // What four matrix instructions take from LDS: of the values at vl, tokens 16 e
+    // + 8 hl + [0, 8) of channels 32 ct + l32; of the keys at kl, channels 16 e + 8
+    // hl + [0, 8), e = 2 g and 2 g + 1, of 32 tokens twice.  (Row r of the logits'
+    // product is token (r & 16) + 8 (r / 4 & 1) + 4 (r / 8 & 1) + r % 4.)
+    static __device__ __forceinline__ void read_v(const uint8_t *vl, int lane, int e, uint4 (&x)[4]) {
+        const int l32 = lane & 31, hl = lane >> 5;
+        const uint8_t *at = vl + l32 * 128 + ((16 * (hl ^ ((l32 >> 1) & 7))) ^ (32 * e));
+#pragma unroll
+        for (int ct = 0; ct < 4; ++ct) x[ct] = *(const uint4 *)(at + 4096 * ct);
+    }
+    static __device__ __forceinline__ void read_k(const uint8_t *kl, int lane, int g, uint4 (&x)[4]) {
         const int l32 = lane & 31, hl = lane >> 5;
         const int tau = (l32 & 16) + 8 * ((l32 >> 2) & 1) + 4 * ((l32 >> 3) & 1) + (l32 & 3);
-        const uint8_t *row = kl + tau * 256;
-        const int at = 16 * (hl ^ (tau & 15));
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int i = 0; i < 4; ++i) x[i] = *(const uint4 *)(kl + tau * 256 + ((16 * (hl ^ (tau & 15))) ^ (32 * (2 * g + (i >> 1)))) + 8192 * (i & 1));
+    }
+    __device__ __forceinline__ void mul_v(const uint4 (&x)[4], uint4 p) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[n][i] = 0.0f;
+        for (int ct = 0; ct < 4; ++ct) acc[ct] = mma32<DT>(x[ct], p, acc[ct]);
+    }
+    __device__ __forceinline__ void mul_k(const uint4 (&x)[4], int g, cf16 (&z)[2]) const {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[n] = mma32<DT>(*(const uint4 *)(row + (at ^ (32 * e)) + 8192 * n), qf[e], z[n]);
+        for (int i = 0; i < 4; ++i) z[i & 1] = mma32<DT>(x[i], qf[2 * g + (i >> 1)], z[i & 1]);
+    }
+    // outputs of the weights pf over the values at vl, and the logits z[n][i] of token 32 n + 16 (i / 8) + 8 hl + i % 8 of
+    // the keys at kl; what an instruction takes is read while the four before it run
+    template <bool V, bool K> __device__ __forceinline__ void multiply(const uint8_t *vl, const uint4 (&pf)[4], const uint8_t *kl, int lane, cf16 (&z)[2]) {
+        uint4 x[2][4];
+        if (V) read_v(vl, lane, 0, x[0]); else read_k(kl, lane, 0, x[0]);
+        if (K)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[n][i] = 0.0f;
+#pragma unroll
+        for (int g = V ? 0 : 4; g < (K ? 8 : 4); ++g) {
+            if (g + 1 < 4) read_v(vl, lane, g + 1, x[(g + 1) & 1]);
+            else if (g + 1 < (K ? 8 : 4)) read_k(kl, lane, g + 1 - 4, x[(g + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (g < 4) mul_v(x[g & 1], pf[g]); else mul_k(x[g & 1], g - 4, z);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     // the softmax's step: weights of tokens 16 e + 8 hl + [0, 8), dealt
@@ -300,15 +331,6 @@ template <int DT> struct Rows {
                                pack16<DT>(x[deal<DT>(4)], x[deal<DT>(5)]), pack16<DT>(x[deal<DT>(6)], x[deal<DT>(7)]));
         }
     }
-    __device__ __forceinline__ void add(uint8_t *vl, int lane, const uint4 (&pf)[4]) {
-        const int l32 = lane & 31, hl = lane >> 5;
-        const uint8_t *row = vl + l32 * 128;
-        const int at = 16 * (hl ^ ((l32 >> 1) & 7));
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[ct] = mma32<DT>(*(const uint4 *)(row + (at ^ (32 * e)) + 4096 * ct), pf[e], acc[ct]);
-    }
 };
 
 __device__ __forceinline__ float share_of(float s) { return s > 0.0f ? 1.0f / s : (s != s ? s : 0.0f); }
@@ -323,7 +345,7 @@ template <int B, int DT, int RW>
 __global__ void __launch_bounds__(64 * RW) __attribute__((amdgpu_waves_per_eu(2)))
 k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
     constexpr int KB = CK_TILE * D * 2;                    // bytes of a step's keys, and of its values
-    __shared__ __align__(16) uint8_t lds[2][2 * KB];
+    __shared__ __align__(16) uint8_t kl[2][KB], vl[2][KB];
     const int id = blockIdx.x / ns, split = blockIdx.x - id * ns;
     const ChunkPlan pl = chunk_plan(q, c, id, tiles, 32 * RW, ns);
     if (pl.row0 >= pl.m * q.G) return;
@@ -334,26 +356,34 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
     const int all = c.causal ? pl.L - pl.m + pl.row0 / q.G + 1 : pl.L;     // tokens that every row of the workgroup attends
     const int whole = pl.L / B, tail = pl.L % B;
     const uint64_t pb = (uint64_t)pl.p * q.N;
-    Step<B, DT, 64 * RW> st;
-    auto load = [&](int t) { st.load_k(q, pb, whole, t, tid); st.load_v(q, pb, whole, t, tid); };
-    auto store = [&](int t, int b) { st.store_k(q, pl.p, pb, whole, tail, t, tid, lds[b]); st.store_v(q, pl.p, pb, whole, tail, t, tid, lds[b] + KB); };
+    constexpr bool TWO = RW == 8;
+    const bool late = TWO && wave >= 4;
+    const int n = t1 - t0, gt = tid & 255;
+    Step<B, DT, 256> st;
+    auto load = [&](int j) {
+        if (j >= n) return;
+        if (!late) st.load_k(q, pb, whole, t0 + j, gt);
+        if (!TWO || late) st.load_v(q, pb, whole, t0 + j, gt);
+    };
+    auto store = [&](int j) {
+        if (j >= n) return;
+        if (!late) st.store_k(q, pl.p, pb, whole, tail, t0 + j, gt, kl[j & 1]);
+        if (!TWO || late) st.store_v(q, pl.p, pb, whole, tail, t0 + j, gt, vl[j & 1]);
+    };
     Rows<DT> r;
-    if (t0 < t1) load(t0);
+    load(0);
     r.begin(q, c, pl, row, hl);
-    if (t0 < t1) store(t0, 0);
-    if (t0 + 1 < t1) load(t0 + 1);
-    for (int t = t0; t < t1; ++t) {
-        const int b = (t - t0) & 1;
-        lds_barrier();                                     // this step's are there, the last one's have been read
+    store(0);
+    load(1);
+    for (int i = 0; i < n; ++i) {
         cf16 z[2];
         uint4 pf[4];
-        r.logits(lds[b], lane, z);
-        if (t + 1 < t1) {
-            store(t + 1, b ^ 1);
-            if (t + 2 < t1) load(t + 2);
-        }
-        r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
-        r.add(lds[b] + KB, lane, pf);
+        lds_barrier();
+        if (late) { store(i + 1); load(i + 2); }
+        r.template multiply<false, true>(nullptr, pf, kl[i & 1], lane, z);
+        if (!late) { store(i + 1); load(i + 2); }
+        r.weigh(z, t0 + i, hl, CK_TILE * (t0 + i + 1) > all, pf);
+        r.template multiply<true, false>(vl[i & 1], pf, nullptr, lane, z);
     }
     const float l = halves(r.l_run, [](float a, float b) { return a + b; }), inv = share_of(l);
     if (pl.used <= 1) {
@@ -408,7 +438,7 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
         mem_fence_compiler();
         wave_sync();
         if (t + W < t1) st.load_k(q, pb, whole, t + W, lane);
-        r.logits(mine, lane, z);
+        r.template multiply<false, true>(nullptr, pf, mine, lane, z);
         mem_fence_compiler();
         wave_sync();
         st.store_v(q, pl.p, pb, whole, tail, t, lane, mine);   // (the wave's LDS operations run in their order)
@@ -416,7 +446,7 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
         wave_sync();
         if (t + W < t1) st.load_v(q, pb, whole, t + W, lane);
         r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
-        r.add(mine, lane, pf);
+        r.template multiply<true, false>(mine, pf, nullptr, lane, z);
         mem_fence_compiler();
         wave_sync();
     }
