@@ -12,11 +12,8 @@
 // product's rows as the second one asks for them, its weights go into the
 // second product without leaving their lanes.
 //
-// Rows are many or few.  Many: all waves of a workgroup share 64 tokens.  A
-// wave's step is a turn on the matrix cores (O of step i, S of step i + 1) and
-// one on the vector ALU (the softmax of step i + 1, its part of later steps
-// worked out into LDS); of the two waves on a SIMD one takes the first kind of
-// turn while the other takes the second.  At most 32 (k_chunk_few): each
+// Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
+// out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
 // wave takes 64 tokens of its own, keys and values one after the other in LDS of
 // its own, and they are joined at the end.  Where there are too few rows for the
 // chip the tokens are split over workgroups, which k_chunk_join joins.
@@ -130,94 +127,93 @@ __device__ __forceinline__ ChunkPlan chunk_plan(const Q4Cache &q, const QChunk &
     return r;
 }
 
-// A step's 64 tokens worked out by GT threads (thread gt): keys at kl by token,
-// rows of 256 bytes, values at vl by channel, rows of 128, both with the 16-byte
-// pieces of a row turned so that the operands' reads spread over the banks.
-template <int B, int DT, int GT> struct Step {
-    static constexpr int KR = GT / 16, KP = CK_TILE / KR;  // keys: tokens of a pass, passes
-    static constexpr int VR = GT / 8, VP = D / VR;         // values: channels of a pass, passes
+// A step's 64 keys (VALS: values) worked out by GT threads (thread gt) into LDS at
+// `to`: keys by token, rows of 256 bytes, values by channel, rows of 128, with the
+// 16-byte pieces of a row turned so that the operands' reads spread over the
+// banks.  A thread takes eight codes a pass: channels 8 (gt % 16) + [0, 8) of a
+// token, or tokens 8 (gt % 8) + [0, 8) of a channel.
+template <int B, int DT, int GT, bool VALS> struct Step {
+    static constexpr int R = VALS ? GT / 8 : GT / 16;      // channels or tokens of a pass
+    static constexpr int P = (VALS ? D : CK_TILE) / R;     // passes
     static constexpr int NB = CK_TILE / B;                 // blocks of a step
-    uint32_t kq[KP], vq[VP];
-    uint4 kg[NB][2], vg[2];
-    static __device__ __forceinline__ uint4 *k_at(uint8_t *kl, int t, int piece) { return (uint4 *)(kl + t * 256 + 16 * (piece ^ (t & 15))); }
-    static __device__ __forceinline__ uint4 *v_at(uint8_t *vl, int ch, int piece) { return (uint4 *)(vl + ch * 128 + 16 * (piece ^ ((ch >> 1) & 7))); }
-    // codes and grids of step t, if its blocks are whole
-    __device__ __forceinline__ void load_k(const Q4Cache &q, uint64_t pb, int whole, int t, int gt) {
-        if (NB * (t + 1) > whole) return;
-        const uint64_t blk = pb + (uint32_t)(NB * t);
+    static constexpr int NG = VALS ? 1 : NB;               // grids of a thread
+    static constexpr int GB = VALS ? 4 * B : 4 * D;        // bytes of a block's grids
+    uint32_t c[P];
+    uint4 g[NG][2];
+    static __device__ __forceinline__ uint4 *at(uint8_t *to, int row, int piece) {
+        return (uint4 *)(VALS ? to + row * 128 + 16 * (piece ^ ((row >> 1) & 7)) : to + row * 256 + 16 * (piece ^ (row & 15)));
+    }
+    // Codes and grids of step t; of one whose blocks are not whole, zeros.  (Through
+    // buffer descriptors: a step is scalar work, and there is no branch, at whose end
+    // the compiler would wait for what was loaded.  2048 queries 1124 us with the
+    // addresses in vector registers, 898 without loads.)
+    __device__ __forceinline__ void load(const Q4Cache &q, uint64_t pb, int whole, int t, int gt) {
+        const bool live = NB * (t + 1) <= whole;
+        const uint64_t blk = pb + (live ? (uint32_t)(NB * t) : 0u);
+        const auto codes = __builtin_amdgcn_make_buffer_rsrc((VALS ? q.v : q.k) + blk * (B * D / 2), 0, live ? CK_TILE * D / 2 : 0, 0x27000);
+        const auto grids = __builtin_amdgcn_make_buffer_rsrc((uint8_t *)(VALS ? q.vg : q.kg) + blk * GB, 0, live ? NB * GB : 0, 0x27000);
+        const int tok = 8 * (gt & 7), b = VALS ? tok / B : 0, ag = VALS ? b * GB + 2 * (tok % B) : 16 * (gt & 15);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const uint16_t *g = q.kg + (blk + b) * (2 * D) + 8 * (gt & 15);
-            kg[b][0] = *(const uint4 *)g;
-            kg[b][1] = *(const uint4 *)(g + D);
+        for (int i = 0; i < NG; ++i) {
+            g[i][0] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(grids, ag + GB * i, 0, 0));
+            g[i][1] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(grids, ag + GB * i + GB / 2, 0, 0));
         }
-        // (blocks lie one after the other, and so do their tokens)
-        const uint8_t *kp = q.k + blk * (B * D / 2) + 4 * gt;
+        const int ac = VALS ? b * (B * D / 2) + (gt >> 3) * (B / 2) + (tok % B) / 2 : 4 * gt;
 #pragma unroll
-        for (int i = 0; i < KP; ++i) kq[i] = *(const uint32_t *)(kp + 4 * GT * i);
+        for (int i = 0; i < P; ++i) c[i] = __builtin_amdgcn_raw_buffer_load_b32(codes, ac + (VALS ? R * (B / 2) : 4 * GT) * i, 0, 0);
     }
-    __device__ __forceinline__ void load_v(const Q4Cache &q, uint64_t pb, int whole, int t, int gt) {
-        if (NB * (t + 1) > whole) return;
-        const int vo = gt & 7, at = 8 * vo % B;
-        const uint64_t blk = pb + (uint32_t)(NB * t + 8 * vo / B);
-        vg[0] = *(const uint4 *)(q.vg + blk * (2 * B) + at);
-        vg[1] = *(const uint4 *)(q.vg + blk * (2 * B) + B + at);
-        const uint8_t *vp = q.v + blk * (B * D / 2) + (gt >> 3) * (B / 2) + at / 2;
+    // a step of whole blocks
+    __device__ __forceinline__ void store_full(int gt, uint8_t *to) const {
 #pragma unroll
-        for (int i = 0; i < VP; ++i) vq[i] = *(const uint32_t *)(vp + VR * (B / 2) * i);
+        for (int b = 0; b < NG; ++b) {
+            const Grid8<DT> gr(g[b][0], g[b][1]);
+#pragma unroll
+            for (int i = b * (P / NG); i < (b + 1) * (P / NG); ++i)
+                *at(to, (VALS ? gt >> 3 : gt >> 4) + R * i, VALS ? gt & 7 : gt & 15) = gr.values(c[i]);
+        }
     }
-    // into LDS; the last step, with tokens of no whole block, is read here one
-    // pass after the other, and tokens past the last are zeros
-    __device__ __forceinline__ void store_k(const Q4Cache &q, int p, uint64_t pb, int whole, int tail, int t, int gt, uint8_t *kl) const {
-        const int kc = gt & 15;
+    // any step; the last one, with tokens of no whole block, is read here one pass
+    // after the other, and tokens past the last are zeros
+    __device__ __forceinline__ void store(const Q4Cache &q, int p, uint64_t pb, int whole, int tail, int t, int gt, uint8_t *to) const {
         if (NB * (t + 1) <= whole) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const Grid8<DT> g(kg[b][0], kg[b][1]);
-#pragma unroll
-                for (int i = b * (KP / NB); i < (b + 1) * (KP / NB); ++i) *k_at(kl, (gt >> 4) + KR * i, kc) = g.values(kq[i]);
-            }
+            store_full(gt, to);
             return;
         }
+        if constexpr (!VALS) {
+            const int kc = gt & 15;
 #pragma unroll 1
-        for (int tk = gt >> 4; tk < CK_TILE; tk += KR) {
-            const int b = NB * t + tk / B;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (b < whole) {
-                const uint64_t blk = pb + (uint32_t)b;
-                const uint16_t *g = q.kg + blk * (2 * D) + 8 * kc;
-                x = Grid8<DT>(*(const uint4 *)g, *(const uint4 *)(g + D)).values(*(const uint32_t *)(q.k + blk * (B * D / 2) + (tk % B) * (D / 2) + 4 * kc));
-            } else if (b == whole && tk % B < tail) {
-                x = dealt<DT>(*(const uint4 *)(q.kt + ((uint64_t)p * B + tk % B) * D + 8 * kc));
+            for (int tk = gt >> 4; tk < CK_TILE; tk += R) {
+                const int b = NB * t + tk / B;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (b < whole) {
+                    const uint64_t blk = pb + (uint32_t)b;
+                    const uint16_t *s = q.kg + blk * (2 * D) + 8 * kc;
+                    x = Grid8<DT>(*(const uint4 *)s, *(const uint4 *)(s + D)).values(*(const uint32_t *)(q.k + blk * (B * D / 2) + (tk % B) * (D / 2) + 4 * kc));
+                } else if (b == whole && tk % B < tail) {
+                    x = dealt<DT>(*(const uint4 *)(q.kt + ((uint64_t)p * B + tk % B) * D + 8 * kc));
+                }
+                *at(to, tk, kc) = x;
             }
-            *k_at(kl, tk, kc) = x;
-        }
-    }
-    __device__ __forceinline__ void store_v(const Q4Cache &q, int p, uint64_t pb, int whole, int tail, int t, int gt, uint8_t *vl) const {
-        const int vo = gt & 7, b = NB * t + 8 * vo / B, at = 8 * vo % B;
-        if (NB * (t + 1) <= whole) {
-            const Grid8<DT> g(vg[0], vg[1]);
-#pragma unroll
-            for (int i = 0; i < VP; ++i) *v_at(vl, (gt >> 3) + VR * i, vo) = g.values(vq[i]);
-            return;
-        }
+        } else {
+            const int vo = gt & 7, b = NB * t + 8 * vo / B, pos = 8 * vo % B;
 #pragma unroll 1
-        for (int ch = gt >> 3; ch < D; ch += VR) {
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (b < whole) {
-                const uint64_t blk = pb + (uint32_t)b;
-                const uint16_t *g = q.vg + blk * (2 * B) + at;
-                x = Grid8<DT>(*(const uint4 *)g, *(const uint4 *)(g + B)).values(*(const uint32_t *)(q.v + blk * (B * D / 2) + ch * (B / 2) + at / 2));
-            } else if (b == whole) {
-                const int keep = tail - at;                // tokens of the eight
-                if (keep > 0) x = *(const uint4 *)(q.vt + ((uint64_t)p * D + ch) * B + at);
-                x.x = keep >= 2 ? x.x : (keep == 1 ? x.x & 0xffffu : 0u);
-                x.y = keep >= 4 ? x.y : (keep == 3 ? x.y & 0xffffu : 0u);
-                x.z = keep >= 6 ? x.z : (keep == 5 ? x.z & 0xffffu : 0u);
-                x.w = keep >= 8 ? x.w : (keep == 7 ? x.w & 0xffffu : 0u);
-                x = dealt<DT>(x);
+            for (int ch = gt >> 3; ch < D; ch += R) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (b < whole) {
+                    const uint64_t blk = pb + (uint32_t)b;
+                    const uint16_t *s = q.vg + blk * (2 * B) + pos;
+                    x = Grid8<DT>(*(const uint4 *)s, *(const uint4 *)(s + B)).values(*(const uint32_t *)(q.v + blk * (B * D / 2) + ch * (B / 2) + pos / 2));
+                } else if (b == whole) {
+                    const int keep = tail - pos;           // tokens of the eight
+                    if (keep > 0) x = *(const uint4 *)(q.vt + ((uint64_t)p * D + ch) * B + pos);
+                    x.x = keep >= 2 ? x.x : (keep == 1 ? x.x & 0xffffu : 0u);
+                    x.y = keep >= 4 ? x.y : (keep == 3 ? x.y & 0xffffu : 0u);
+                    x.z = keep >= 6 ? x.z : (keep == 5 ? x.z & 0xffffu : 0u);
+                    x.w = keep >= 8 ? x.w : (keep == 7 ? x.w & 0xffffu : 0u);
+                    x = dealt<DT>(x);
+                }
+                *at(to, ch, vo) = x;
             }
-            *v_at(vl, ch, vo) = x;
         }
     }
 };
@@ -356,34 +352,59 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
     const int all = c.causal ? pl.L - pl.m + pl.row0 / q.G + 1 : pl.L;     // tokens that every row of the workgroup attends
     const int whole = pl.L / B, tail = pl.L % B;
     const uint64_t pb = (uint64_t)pl.p * q.N;
+    // Of eight waves the first four work out the keys, the others the values, before
+    // the logits rather than after them, so that a SIMD's two waves differ.  Four
+    // waves do both.  The first loop has no branch: its steps are whole, and every
+    // row sees them.
     constexpr bool TWO = RW == 8;
-    const bool late = TWO && wave >= 4;
     const int n = t1 - t0, gt = tid & 255;
-    Step<B, DT, 256> st;
-    auto load = [&](int j) {
-        if (j >= n) return;
-        if (!late) st.load_k(q, pb, whole, t0 + j, gt);
-        if (!TWO || late) st.load_v(q, pb, whole, t0 + j, gt);
-    };
-    auto store = [&](int j) {
-        if (j >= n) return;
-        if (!late) st.store_k(q, pl.p, pb, whole, tail, t0 + j, gt, kl[j & 1]);
-        if (!TWO || late) st.store_v(q, pl.p, pb, whole, tail, t0 + j, gt, vl[j & 1]);
-    };
     Rows<DT> r;
-    load(0);
     r.begin(q, c, pl, row, hl);
-    store(0);
-    load(1);
-    for (int i = 0; i < n; ++i) {
+    auto work = [&](auto values_first) {
+        constexpr bool VALS = decltype(values_first)::value;
+        Step<B, DT, 256, VALS> st;
+        Step<B, DT, 256, true> sv;                         // (four waves' values)
+        auto load = [&](int i) {
+            const int t = t0 + min(i, n - 1);
+            st.load(q, pb, whole, t, gt);
+            if (!TWO) sv.load(q, pb, whole, t, gt);
+        };
+        auto store = [&](int i) {
+            if (i >= n) return;
+            st.store(q, pl.p, pb, whole, tail, t0 + i, gt, VALS ? vl[i & 1] : kl[i & 1]);
+            if (!TWO) sv.store(q, pl.p, pb, whole, tail, t0 + i, gt, vl[i & 1]);
+        };
+        auto store_full = [&](int i) {
+            st.store_full(gt, VALS ? vl[i & 1] : kl[i & 1]);
+            if (!TWO) sv.store_full(gt, vl[i & 1]);
+        };
         cf16 z[2];
         uint4 pf[4];
-        lds_barrier();
-        if (late) { store(i + 1); load(i + 2); }
-        r.template multiply<false, true>(nullptr, pf, kl[i & 1], lane, z);
-        if (!late) { store(i + 1); load(i + 2); }
-        r.weigh(z, t0 + i, hl, CK_TILE * (t0 + i + 1) > all, pf);
-        r.template multiply<true, false>(vl[i & 1], pf, nullptr, lane, z);
+        load(0);
+        store(0);
+        load(1);
+        int i = 0;
+        const int plain = min(min(n - 1, whole * B / CK_TILE - t0 - 1), all / CK_TILE - t0);
+        for (; i < plain; ++i) {
+            lds_barrier();
+            if (VALS) { store_full(i + 1); load(i + 2); }
+            r.template multiply<false, true>(nullptr, pf, kl[i & 1], lane, z);
+            if (!VALS) { store_full(i + 1); load(i + 2); }
+            r.weigh(z, t0 + i, hl, false, pf);
+            r.template multiply<true, false>(vl[i & 1], pf, nullptr, lane, z);
+        }
+        for (; i < n; ++i) {
+            lds_barrier();
+            if (VALS) { store(i + 1); load(i + 2); }
+            r.template multiply<false, true>(nullptr, pf, kl[i & 1], lane, z);
+            if (!VALS) { store(i + 1); load(i + 2); }
+            r.weigh(z, t0 + i, hl, CK_TILE * (t0 + i + 1) > all, pf);
+            r.template multiply<true, false>(vl[i & 1], pf, nullptr, lane, z);
+        }
+    };
+    if (n > 0) {
+        if (TWO && wave >= 4) work(std::true_type{});
+        else work(std::false_type{});
     }
     const float l = halves(r.l_run, [](float a, float b) { return a + b; }), inv = share_of(l);
     if (pl.used <= 1) {
@@ -426,25 +447,27 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
     const int whole = pl.L / B, tail = pl.L % B;
     const uint64_t pb = (uint64_t)pl.p * q.N;
     uint8_t *mine = lds[wave];
-    Step<B, DT, 64> st;
+    Step<B, DT, 64, false> sk;
+    Step<B, DT, 64, true> sv;
     int t = t0 + wave;
-    if (t < t1) { st.load_k(q, pb, whole, t, lane); st.load_v(q, pb, whole, t, lane); }
+    sk.load(q, pb, whole, t, lane);
+    sv.load(q, pb, whole, t, lane);
     Rows<DT> r;
     r.begin(q, c, pl, l32, hl);
     for (; t < t1; t += W) {
         cf16 z[2];
         uint4 pf[4];
-        st.store_k(q, pl.p, pb, whole, tail, t, lane, mine);
+        sk.store(q, pl.p, pb, whole, tail, t, lane, mine);
         mem_fence_compiler();
         wave_sync();
-        if (t + W < t1) st.load_k(q, pb, whole, t + W, lane);
+        sk.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
         r.template multiply<false, true>(nullptr, pf, mine, lane, z);
         mem_fence_compiler();
         wave_sync();
-        st.store_v(q, pl.p, pb, whole, tail, t, lane, mine);   // (the wave's LDS operations run in their order)
+        sv.store(q, pl.p, pb, whole, tail, t, lane, mine);   // (the wave's LDS operations run in their order)
         mem_fence_compiler();
         wave_sync();
-        if (t + W < t1) st.load_v(q, pb, whole, t + W, lane);
+        sv.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
         r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
         r.template multiply<true, false>(mine, pf, nullptr, lane, z);
         mem_fence_compiler();
