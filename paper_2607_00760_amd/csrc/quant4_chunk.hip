@@ -288,6 +288,27 @@ template <int DT> struct Rows {
             __builtin_amdgcn_sched_barrier(0);
         }
     }
+    // the same, read as the compiler sees fit (fewer registers)
+    __device__ __forceinline__ void multiply_v(const uint8_t *vl, const uint4 (&pf)[4], int lane) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint4 x[4];
+            read_v(vl, lane, e, x);
+            mul_v(x, pf[e]);
+        }
+    }
+    __device__ __forceinline__ void multiply_k(const uint8_t *kl, int lane, cf16 (&z)[2]) const {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[n][i] = 0.0f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            uint4 x[4];
+            read_k(kl, lane, g, x);
+            mul_k(x, g, z);
+        }
+    }
     // the softmax's step: weights of tokens 16 e + 8 hl + [0, 8), dealt
     __device__ __forceinline__ void weigh(cf16 (&z)[2], int t, int hl, bool masked, uint4 (&pf)[4]) {
         if (masked) {
@@ -461,7 +482,7 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
         mem_fence_compiler();
         wave_sync();
         sk.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
-        r.template multiply<false, true>(nullptr, pf, mine, lane, z);
+        r.multiply_k(mine, lane, z);
         mem_fence_compiler();
         wave_sync();
         sv.store(q, pl.p, pb, whole, tail, t, lane, mine);   // (the wave's LDS operations run in their order)
@@ -469,7 +490,7 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
         wave_sync();
         sv.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
         r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
-        r.template multiply<true, false>(mine, pf, nullptr, lane, z);
+        r.multiply_v(mine, pf, lane);
         mem_fence_compiler();
         wave_sync();
     }
