@@ -58,15 +58,17 @@ __device__ __forceinline__ dbf8 k_codes(uint32_t w) {
 __device__ __forceinline__ constexpr int k_order(int i) { return (2 * i & 7) + (i >> 2); }
 
 // the codes of w less 8 as fp16, in the order 0, 4, 1, 5, 2, 6, 3, 7
-__device__ __forceinline__ dhf8 v_codes(uint32_t w) {
+// (`base`: 0x64006400 from a vector register, as one instruction takes its mask
+// and its other constant from nowhere else.)
+__device__ __forceinline__ dhf8 v_codes(uint32_t w, uint32_t base) {
     typedef __attribute__((ext_vector_type(2))) _Float16 h2;
     const h2 off = {(_Float16)1032.0f, (_Float16)1032.0f}, by = {(_Float16)0.0625f, (_Float16)0.0625f}, off16 = {(_Float16)-72.0f, (_Float16)-72.0f};
     h2 o[4];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const uint32_t u = e ? w >> 8 : w;
-        o[2 * e] = __builtin_bit_cast(h2, (u & 0x000f000fu) | 0x64006400u) - off;
-        o[2 * e + 1] = __builtin_elementwise_fma(__builtin_bit_cast(h2, (u & 0x00f000f0u) | 0x64006400u), by, off16);
+        o[2 * e] = __builtin_bit_cast(h2, (u & 0x000f000fu) | base) - off;
+        o[2 * e + 1] = __builtin_elementwise_fma(__builtin_bit_cast(h2, (u & 0x00f000f0u) | base), by, off16);
     }
     dhf8 r;
     __builtin_memcpy(&r, o, 16);
@@ -126,7 +128,12 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
 #pragma unroll
     for (int e = 0; e < 4; ++e) qw[e] = *(const uint4 *)(qp + 32 * q4 + 8 * e);
     if (t < b1) load(t, st0);
-    const float zs = scale * 1.44269504088896340736f;      // softmax scale in powers of two
+    // softmax scale in powers of two, positive (a negative one's sign goes to the
+    // query), as logits are scaled when their maximum is known
+    const float zs = fmaxf(fabsf(scale) * 1.44269504088896340736f, 0x1p-120f);
+    const uint32_t flip = scale < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) qw[e] = make_uint4(qw[e].x ^ flip, qw[e].y ^ flip, qw[e].z ^ flip, qw[e].w ^ flip);
     // the part of the query's products that the lane's column holds
     const int mypart = GP == 8 ? l16 >> 3 : (DT ? (l16 >> 2) & 1 : l16 >> 2);
     const uint32_t qh1 = mypart >= 1 ? 0xffff0000u : 0u, qh2 = mypart >= 2 ? 0xffff0000u : 0u, qh3 = mypart >= 3 ? 0u : ~0u;
@@ -137,6 +144,8 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
     auto expo = [](float x) { return max(__float_as_uint(x) >> 23, PS + 1u); };
     auto unit = [&](float x) { return __uint_as_float((expo(x) - PS) << 23); };
     auto per_unit = [&](float x) { return __uint_as_float((254u + PS - expo(x)) << 23); };
+    uint32_t base = 0x64006400u;
+    asm volatile("" : "+v"(base));
     df4 acc[8];                                            // [channel tile][row 4 q4 + r]
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) acc[ct] = df4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -151,19 +160,19 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
         cm = rows_all(cm, [](float a, float b) { return fmaxf(a, b); });
         const float mn = fmaxf(m_run, cm);
         const float mb = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - mb);
+        const float mz = -mb * zs, alpha = __builtin_amdgcn_exp2f((m_run - mb) * zs);
         float ls = 0.0f;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                z[n][r] = __builtin_amdgcn_exp2f(z[n][r] - mb);
+                z[n][r] = __builtin_amdgcn_exp2f(fmaf(z[n][r], zs, mz));
                 ls += z[n][r];
             }
         l_run = fmaf(l_run, alpha, ls);
         m_run = mn;
         const float was = unit(top);
-        top = fmaxf(fmaxf(top * alpha, __builtin_amdgcn_exp2f(cm - mb) * reach) * low, least);
+        top = fmaxf(fmaxf(top * alpha, __builtin_amdgcn_exp2f((cm - mb) * zs) * reach) * low, least);
         const float per = per_unit(top), grow = alpha * was * per;
         shift *= grow;
         if (!__all(grow == 1.0f)) {                        // some head's running maximum or unit moved
@@ -199,14 +208,14 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
         mem_fence_compiler();
         wave_sync();
         dbf8 qa[4], qt[4];                                 // the query's products with the block's scales
-        df4 base = df4{0.0f, 0.0f, 0.0f, 0.0f};            // what the zeros add
+        df4 zq = df4{0.0f, 0.0f, 0.0f, 0.0f};              // what the zeros add
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint4 ks = lg[4 * q4 + e], kz = lg[D / 8 + 4 * q4 + e];
             M8 zo, qo;
             __builtin_memcpy(&zo, &kz, 16);
             __builtin_memcpy(&qo, &qw[e], 16);
-            base = DM::run(zo, qo, base);
+            zq = DM::run(zo, qo, zq);
             float x[8], y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -225,11 +234,11 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
             if (THIRD) qt[e] = upper_halves(y);
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) base[r] = mypart == 0 ? base[r] : 0.0f;
+        for (int r = 0; r < 4; ++r) zq[r] = mypart == 0 ? zq[r] : 0.0f;
         float z[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            df4 a = base;
+            df4 a = zq;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const dbf8 c = k_codes(words(&st.k[n])[e]);
@@ -241,7 +250,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
                 float s = a[r];
                 if (GP == 8 || !DT) s = ror_add<8>(s);
                 if (GP == 4) s = ror_add<4>(s);
-                z[n][r] = s * zs;
+                z[n][r] = s;
             }
         }
         uint4 vs[NS], vz[NS];                              // of the lane's tokens
@@ -266,7 +275,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
             }
             const dhf8 pa = split16(w);
 #pragma unroll
-            for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, v_codes(st.v[ct][s]), acc[ct]);
+            for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, v_codes(st.v[ct][s], base), acc[ct]);
         }
     };
     while (t < b1) {                                       // (two steps a turn: no copies that would wait on the loads)
@@ -288,7 +297,11 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
         const uint16_t *kp = q.kt + (uint64_t)p * B * D, *vp = q.vt + (uint64_t)p * B * D;
         M8 qd[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) __builtin_memcpy(&qd[e], qp + 32 * e + 8 * q4, 16);
+        for (int e = 0; e < 4; ++e) {
+            const uint4 w = *(const uint4 *)(qp + 32 * e + 8 * q4);
+            const uint4 f = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
+            __builtin_memcpy(&qd[e], &f, 16);
+        }
         uint4 vt[NS][8];                                   // (rows behind the last token may hold anything)
 #pragma unroll
         for (int s = 0; s < NS; ++s)
@@ -313,7 +326,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
                 a = DM::run(x, qd[e], a);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) z[n][r] = TPQ * q4 + 4 * n + r < rest ? a[r] * zs : -INFINITY;
+            for (int r = 0; r < 4; ++r) z[n][r] = TPQ * q4 + 4 * n + r < rest ? a[r] : -INFINITY;
         }
         // fp16 values are at most 2^16 of a unit and leave their sums room.  bf16
         // ones go up to 2^128, in a bf16 product with three parts of the weights
@@ -368,7 +381,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
     lane &= 63;
     const int row = lane >> 4, col = lane & 15;            // (worked out again, as above)
     if (lane < 16) {                                       // a head's unit and shift stand in the row of its second parts
-        mrg[wave][col][0] = lane < GP ? m_run : unit(top);
+        mrg[wave][col][0] = lane < GP ? m_run * zs : unit(top);
         mrg[wave][col][1] = lane < GP ? l_run : shift;
     }
 #pragma unroll

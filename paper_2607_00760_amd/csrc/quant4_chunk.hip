@@ -90,12 +90,14 @@ template <> struct Grid8<0> {
     // the same in fp16, one rounding (a code's bits under 1024 are 1024 + code)
     __device__ __forceinline__ uint4 values(uint32_t c) const {
         const ch2 off = {(_Float16)1024.0f, (_Float16)1024.0f}, by = {(_Float16)0.0625f, (_Float16)0.0625f}, off16 = {(_Float16)-64.0f, (_Float16)-64.0f};
+        uint32_t base = 0x64006400u;                       // (from a vector register: mask and base in one instruction)
+        asm("" : "+v"(base));
         ch2 o[4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const uint32_t u = e ? c >> 8 : c;
-            const ch2 a = __builtin_bit_cast(ch2, (u & 0x000f000fu) | 0x64006400u) - off;
-            const ch2 b = __builtin_elementwise_fma(__builtin_bit_cast(ch2, (u & 0x00f000f0u) | 0x64006400u), by, off16);
+            const ch2 a = __builtin_bit_cast(ch2, (u & 0x000f000fu) | base) - off;
+            const ch2 b = __builtin_elementwise_fma(__builtin_bit_cast(ch2, (u & 0x00f000f0u) | base), by, off16);
             o[2 * e] = __builtin_elementwise_fma(s[2 * e], a, z[2 * e]);
             o[2 * e + 1] = __builtin_elementwise_fma(s[2 * e + 1], b, z[2 * e + 1]);
         }
