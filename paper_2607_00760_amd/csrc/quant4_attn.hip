@@ -20,9 +20,11 @@
 // fp16 parts in rows [part][head] of the left operand.  So both products are
 // exact up to the sums' fp32 roundings and 2^-23 of a weight.
 //
-// Sums are in units of a power of two that follows the largest product of a
-// weight and a token's scale or zero: weights keep to fp16's range, and bf16
-// values may be of any size.
+// The second sum is in units of a power of two that follows the largest product
+// of a weight and a token's scale, so weights keep to fp16's range however far
+// apart scales are (a unit of the largest weight times the largest scale lost
+// weights of 2^-30 on values 2^40 times as large as the others'); the first is in
+// units of its own, so bf16 values may be of any size.
 #include <type_traits>
 
 #include "quant4.h"
@@ -138,9 +140,9 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
     const int mypart = GP == 8 ? l16 >> 3 : (DT ? (l16 >> 2) & 1 : l16 >> 2);
     const uint32_t qh1 = mypart >= 1 ? 0xffff0000u : 0u, qh2 = mypart >= 2 ? 0xffff0000u : 0u, qh3 = mypart >= 3 ? 0u : ~0u;
     float m_run = -INFINITY, l_run = 0.0f;                 // head l16 % GP; sums over this lane's tokens only
-    float shift = 0.0f;                                    // sum of p zv, in units
-    float top = 0x1p-100f;                                 // the largest product of weight and value grid so far; sums are
-                                                           // in units of the power of two below it, / 2^PS
+    float shift = 0.0f;                                    // sum of p (zv + 8 sv), for bf16 in units of far's power of two
+    float top = 0x1p-100f, far = 0x1p-100f;                // the largest product of a weight and a scale so far, and a bound of
+                                                           // one and a zero; units are the powers of two below them, / 2^PS
     auto expo = [](float x) { return max(__float_as_uint(x) >> 23, PS + 1u); };
     auto unit = [&](float x) { return __uint_as_float((expo(x) - PS) << 23); };
     auto per_unit = [&](float x) { return __uint_as_float((254u + PS - expo(x)) << 23); };
@@ -149,9 +151,9 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
     df4 acc[8];                                            // [channel tile][row 4 q4 + r]
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) acc[ct] = df4{0.0f, 0.0f, 0.0f, 0.0f};
-    // the softmax's step over logits z, to weights; `reach`: the largest scale or
-    // zero of the values.  Returns what takes products to units.
-    auto weigh = [&](float (&z)[NT][4], float reach, float low, float least) {
+    // the softmax's step over logits z, to weights: returns what older sums are
+    // multiplied by, and the largest weight
+    auto weigh = [&](float (&z)[NT][4], float &most) {
         float cm = -INFINITY;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -161,6 +163,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
         const float mn = fmaxf(m_run, cm);
         const float mb = mn == -INFINITY ? 0.0f : mn;
         const float mz = -mb * zs, alpha = __builtin_amdgcn_exp2f((m_run - mb) * zs);
+        most = __builtin_amdgcn_exp2f((cm - mb) * zs);
         float ls = 0.0f;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -171,10 +174,14 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
             }
         l_run = fmaf(l_run, alpha, ls);
         m_run = mn;
+        return alpha;
+    };
+    // the unit of the sums follows to `reach`; returns what takes products to it.
+    // (What follows in 16 bits has room for a smaller unit: low, least.)
+    auto follow = [&](float alpha, float reach, float low, float least) {
         const float was = unit(top);
-        top = fmaxf(fmaxf(top * alpha, __builtin_amdgcn_exp2f((cm - mb) * zs) * reach) * low, least);
+        top = fmaxf(fmaxf(top * alpha, reach) * low, least);
         const float per = per_unit(top), grow = alpha * was * per;
-        shift *= grow;
         if (!__all(grow == 1.0f)) {                        // some head's running maximum or unit moved
             float f[4];
 #pragma unroll
@@ -256,24 +263,42 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
         uint4 vs[NS], vz[NS];                              // of the lane's tokens
 #pragma unroll
         for (int s = 0; s < NS; ++s) { vs[s] = lg[2 * D / 8 + NS * q4 + s]; vz[s] = lg[(2 * D + B) / 8 + NS * q4 + s]; }
-        // the largest scale of the block's tokens, for bf16 also their zeros (fp16's
-        // keep their sum in range)
-        uint32_t m = 0;
+        float most;
+        const float alpha = weigh(z, most);
+        float w[NS][8], mids = 0.0f, reach = 0.0f;
 #pragma unroll
-        for (int i = 0; i < TPQ / 2; ++i) m = pk_umax(m, DT ? pk_umax(words(vs)[i], words(vz)[i] & 0x7fff7fffu) : words(vs)[i]);
-        const float reach = rows_all(fmaxf(half_of<DT>(&m, 0), half_of<DT>(&m, 1)), [](float a, float b) { return fmaxf(a, b); });
-        const float per = weigh(z, reach, 1.0f, 0.0f);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            float w[8];
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int at = v_order(i);
-                const float e = z[2 * s + (at >> 2)][at & 3] * per, sc = half_of<DT>(words(&vs[s]), at);
-                w[i] = e * sc;
-                shift = fmaf(e, fmaf(sc, 8.0f, half_of<DT>(words(&vz[s]), at)), shift);
+                const float e = z[2 * s + (at >> 2)][at & 3], sc = half_of<DT>(words(&vs[s]), at);
+                w[s][i] = e * sc;
+                reach = fmaxf(reach, w[s][i]);
+                if (!DT) mids = fmaf(e, fmaf(sc, 8.0f, half_of<DT>(words(&vz[s]), at)), mids);
             }
-            const dhf8 pa = split16(w);
+        if (DT) {                                          // (the sums of a block, too, could pass fp32's range)
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < TPQ / 2; ++i) m = pk_umax(m, pk_umax(words(vs)[i], words(vz)[i] & 0x7fff7fffu));
+            const float big = rows_all(fmaxf(half_of<DT>(&m, 0), half_of<DT>(&m, 1)), [](float a, float b) { return fmaxf(a, b); });
+            const float was = unit(far);
+            far = fmaxf(far * alpha, most * big);
+            const float per = per_unit(far);
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    mids = fmaf(z[2 * s + (i >> 2)][i & 3] * per, fmaf(half_of<DT>(words(&vs[s]), i), 8.0f, half_of<DT>(words(&vz[s]), i)), mids);
+            shift = fmaf(shift, alpha * was * per, mids);
+        } else {
+            shift = fmaf(shift, alpha, mids);
+        }
+        const float per = follow(alpha, rows_all(reach, [](float a, float b) { return fmaxf(a, b); }), 1.0f, 0.0f);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[s][i] *= per;
+            const dhf8 pa = split16(w[s]);
 #pragma unroll
             for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, v_codes(st.v[ct][s], base), acc[ct]);
         }
@@ -328,11 +353,12 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
 #pragma unroll
             for (int r = 0; r < 4; ++r) z[n][r] = TPQ * q4 + 4 * n + r < rest ? a[r] : -INFINITY;
         }
-        // fp16 values are at most 2^16 of a unit and leave their sums room.  bf16
-        // ones go up to 2^128, in a bf16 product with three parts of the weights
-        // (the third in one of its own): the unit knows the largest, and is 2^60
-        // below it, as the parts would fall below 2^-126 next to the largest values.
-        float reach = 1.0f;
+        // A bf16 product, with three parts of the weights (the third in one of its
+        // own) and two of fp16 values.  fp16 values are at most 2^16 of a unit and
+        // leave their sums room.  bf16 ones go up to 2^128: the unit knows the largest,
+        // and is 2^60 below it, as the parts would fall below 2^-126 next to the
+        // largest values.
+        float reach = 1.0f, most;
         if (DT) {
             float a = 0.0f;
 #pragma unroll
@@ -346,36 +372,49 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
                     }
             reach = __uint_as_float(wave_max_u(__float_as_uint(a)));
         }
-        const float per = DT ? weigh(z, reach, 0x1p-60f, 0x1p-60f) : weigh(z, 1.0f, 1.0f, 0.0f);
+        const float alpha = weigh(z, most);
+        const float per = DT ? follow(alpha, most * reach, 0x1p-60f, 0x1p-60f) : follow(alpha, most, 1.0f, 0.0f);
+        if (DT) {                                          // (shift's unit follows, too)
+            const float was = unit(far);
+            far *= alpha;
+            shift *= alpha * was * per_unit(far);
+        } else {
+            shift *= alpha;
+        }
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-            float w[8];
+            float x[8], y[8];
+            const uint32_t second = (l16 & GP) ? 0xffff0000u : 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = z[2 * s + (i >> 2)][i & 3] * per;
-            if constexpr (DT) {
-                float x[8], y[8];
-                const uint32_t second = (l16 & GP) ? 0xffff0000u : 0u;
+            for (int i = 0; i < 8; ++i) {
+                const float w = z[2 * s + (i >> 2)][i & 3] * per;
+                x[i] = beyond(w, second);
+                y[i] = second ? 0.0f : beyond(beyond(w));
+            }
+            const dbf8 pa = upper_halves(x), third = upper_halves(y);
+            auto add = [&](df4 &a, const dbf8 &vb) {
+                a = DMma<1>::run(pa, vb, a);
+                a = DMma<1>::run(third, vb, a);
+            };
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[i] = beyond(w[i], second);
-                    y[i] = second ? 0.0f : beyond(beyond(w[i]));
+            for (int ct = 0; ct < 8; ++ct) {
+                if (DT) {
+                    add(acc[ct], __builtin_bit_cast(dbf8, vt[s][ct]));
+                } else {
+                    float u[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[i] = half_of<0>(words(&vt[s][ct]), i);
+                    add(acc[ct], upper_halves(u));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) u[i] = beyond(u[i]);
+                    add(acc[ct], upper_halves(u));
                 }
-                const dbf8 pa = upper_halves(x), third = upper_halves(y);
-#pragma unroll
-                for (int ct = 0; ct < 8; ++ct) {
-                    acc[ct] = DMma<1>::run(pa, __builtin_bit_cast(dbf8, vt[s][ct]), acc[ct]);
-                    acc[ct] = DMma<1>::run(third, __builtin_bit_cast(dbf8, vt[s][ct]), acc[ct]);
-                }
-            } else {
-                const dhf8 pa = split16(w);
-#pragma unroll
-                for (int ct = 0; ct < 8; ++ct) acc[ct] = DMma<0>::run(pa, __builtin_bit_cast(dhf8, vt[s][ct]), acc[ct]);
             }
         }
     }
     // join the waves
     l_run = rows_all(l_run, [](float a, float b) { return a + b; });
-    shift = rows_all(shift, [](float a, float b) { return a + b; });
+    shift = rows_all(shift, [](float a, float b) { return a + b; }) * share_of(l_run) * (DT ? unit(far) : 1.0f);   // an average
     int lane = tid;
     asm volatile("" : "+v"(lane));
     lane &= 63;

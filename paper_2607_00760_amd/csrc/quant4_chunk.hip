@@ -477,25 +477,29 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
     sv.load(q, pb, whole, t, lane);
     Rows<DT> r;
     r.begin(q, c, pl, l32, hl);
-    for (; t < t1; t += W) {
+    auto step = [&](auto any) {                            // any: also one whose blocks are not whole
+        constexpr bool ANY = decltype(any)::value;
         cf16 z[2];
         uint4 pf[4];
-        sk.store(q, pl.p, pb, whole, tail, t, lane, mine);
+        if (ANY) sk.store(q, pl.p, pb, whole, tail, t, lane, mine); else sk.store_full(lane, mine);
         mem_fence_compiler();
         wave_sync();
-        sk.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
+        if (!ANY) sk.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
         r.multiply_k(mine, lane, z);
         mem_fence_compiler();
         wave_sync();
-        sv.store(q, pl.p, pb, whole, tail, t, lane, mine);   // (the wave's LDS operations run in their order)
+        if (ANY) sv.store(q, pl.p, pb, whole, tail, t, lane, mine); else sv.store_full(lane, mine);
         mem_fence_compiler();
-        wave_sync();
-        sv.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
+        wave_sync();                                       // (the wave's LDS operations run in their order)
+        if (!ANY) sv.load(q, pb, whole, t + W < t1 ? t + W : t, lane);
         r.weigh(z, t, hl, CK_TILE * (t + 1) > all, pf);
         r.multiply_v(mine, pf, lane);
         mem_fence_compiler();
         wave_sync();
-    }
+    };
+    const int full = min(t1, whole * B / CK_TILE);
+    for (; t < full; t += W) step(std::false_type{});
+    if (t < t1) step(std::true_type{});                    // (the last step of all)
     // the waves joined, in their order; each takes 16 channels
     float l = halves(r.l_run, [](float a, float b) { return a + b; });
     float *sums = (float *)mine;                           // [channel][row]

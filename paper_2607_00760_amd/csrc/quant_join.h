@@ -132,7 +132,7 @@ __device__ __forceinline__ dbf8 upper_halves(const float (&x)[8]) {
 // workgroup the runs.  mrg[wave][row]: rows h, GP + h (, 2 GP + h) are the NP parts
 // of head h's sums from column 2 on; (row h, 0) its running maximum, (h, 1) the
 // sum of its weights, (GP + h, 0) the unit of its sums and, with SHIFT, (GP + h,
-// 1) what is added to each of them.
+// 1) what is added to each of its averages.
 template <int GP, int NP, bool SHIFT>
 __device__ __forceinline__ void join_waves(float (&mrg)[QA_NWV][16][D + 2], int &last, const QPlan &pl, int G, int p,
                                            uint32_t *arrivals, float *part, float *outp) {
@@ -164,9 +164,9 @@ __device__ __forceinline__ void join_waves(float (&mrg)[QA_NWV][16][D + 2], int 
                 u.x += v.x;
                 u.y += v.y;
             }
-            if (SHIFT) { u.x += mrg[w][h + GP][1]; u.y += mrg[w][h + GP][1]; }
-            A.x += u.x * fu;
-            A.y += u.y * fu;
+            const float add = SHIFT ? mrg[w][h + GP][1] * (f[w] * mrg[w][h][1] * inv) : 0.0f;
+            A.x += SHIFT ? fmaf(u.x, fu, add) : u.x * fu;
+            A.y += SHIFT ? fmaf(u.y, fu, add) : u.y * fu;
         }
         if (pl.ns == 1) {
             *(float2 *)(out + i) = A;

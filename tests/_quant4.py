@@ -61,7 +61,7 @@ class Pair:
     def spread(self):
         """[n][D]: how large the terms of a key's and a value's products are."""
         def one(parts, raw, turn):
-            whole = [np.abs(z)[:, None] + 31 * s[:, None] + 0 * c for c, s, z in parts]
+            whole = [np.abs(z.astype(np.float64))[:, None] + 31.0 * s.astype(np.float64)[:, None] + 0 * c for c, s, z in parts]
             whole = [w.T if turn else w for w in whole]
             return np.concatenate(whole + [np.abs(raw[self.nb * self.B:])]).astype(np.float64)
         return one(self.kc, self.k, True), one(self.vc, self.v, False)

@@ -1,0 +1,102 @@
+"""Rotations to positions of several axes on the GPU, against fp64."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_00760_amd as M
+
+pytestmark = pytest.mark.gpu
+D = 128
+DT = {"fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+def exact(x, at, inv, w, interleaved, eps=1e-6):
+    """x [S][n][heads][D]; at [S][n][R / 2]: each pair's position.  fp64, and the rows' sizes."""
+    y = x.double()
+    if w is not None:
+        y = y / torch.sqrt((y * y).mean(-1, keepdim=True) + eps) * w.double()
+    t = (at.double() * inv.double())[:, :, None]
+    h = inv.numel()
+    a, b = (y[..., 0: 2 * h: 2], y[..., 1: 2 * h: 2]) if interleaved else (y[..., :h], y[..., h: 2 * h])
+    u, v = a * torch.cos(t) - b * torch.sin(t), b * torch.cos(t) + a * torch.sin(t)
+    z = y.clone()
+    if interleaved:
+        z[..., 0: 2 * h: 2], z[..., 1: 2 * h: 2] = u, v
+    else:
+        z[..., :h], z[..., h: 2 * h] = u, v
+    return z
+
+
+def case(S, n, hq, hkv, dt, rot, A, seed, wide=False):
+    g = torch.Generator().manual_seed(seed)
+    qkv = torch.randn((S, n, hq + 2 * hkv, D), generator=g).to(dt)
+    pos = torch.randint(-(1 << 20) if wide else 0, 1 << (20 if wide else 12), (A, S, n), generator=g)
+    inv = torch.pow(10000.0, -torch.arange(0, rot, 2).double() / rot).float()
+    w = [(1 + 0.2 * torch.randn(D, generator=g)).to(dt) for _ in range(2)]
+    return qkv, pos, inv, w
+
+
+def check(got, want, dt):
+    """One rounding of the result, and four fp32 ones of a pair's larger member."""
+    got, want = got.cpu().double(), want.double()
+    assert ((got - want).abs() <= torch.finfo(dt).eps / 2 * want.abs() * 1.001 + 2.0 ** -20 * want.abs().amax(-1, keepdim=True) + 1e-7).all(), \
+        (got - want).abs().max()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("S,n,hq,hkv,rot,A", [(1, 1, 4, 1, 128, 3), (3, 37, 28, 4, 64, 2), (2, 300, 32, 8, 128, 4), (1, 513, 5, 5, 96, 1), (2, 5, 8, 8, 16, 7)])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_axes(dtype, S, n, hq, hkv, rot, A, norm, interleaved):
+    dt = DT[dtype]
+    qkv, pos, inv, w = case(S, n, hq, hkv, dt, rot, A, 60)
+    ws = w if norm else (None, None)
+    x = qkv.cuda()
+    for axes in ([i * A // (rot // 2) for i in range(rot // 2)], [i % A for i in range(rot // 2)], [A - 1] * (rot // 2)):
+        at = pos[torch.tensor(axes)].permute(1, 2, 0)
+        q, k, v = M.qk_norm_rope(x[:, :, :hq], x[:, :, hq: hq + hkv], pos.cuda(), inv.cuda(), *[None if t is None else t.cuda() for t in ws],
+                                 interleaved=interleaved, v=x[:, :, hq + hkv:], axes=axes)
+        check(q, exact(qkv[:, :, :hq], at, inv, ws[0], interleaved), dt)
+        check(k.transpose(1, 2), exact(qkv[:, :, hq: hq + hkv], at, inv, ws[1], interleaved), dt)
+        assert torch.equal(v.transpose(1, 2).cpu(), qkv[:, :, hq + hkv:])
+
+
+@pytest.mark.parametrize("kind", [torch.int32, torch.int64])
+def test_strides_and_kinds_of_positions(kind):
+    """Positions of any strides (shared by sequences, by axes), wide ones; the
+    axes as a list, a tuple, bytes or an array."""
+    S, n, hq, hkv, dt = 3, 50, 4, 2, torch.float16
+    qkv, pos, inv, w = case(S, n, hq, hkv, dt, 128, 3, 61, wide=True)
+    x, axes = qkv.cuda(), [i % 3 for i in range(64)]
+    turned = torch.empty((n, 3, S), dtype=kind, device="cuda").permute(1, 2, 0).copy_(pos)
+    for p in (pos.to(kind).cuda(), turned, pos[:, :1].to(kind).cuda().expand(3, S, n), pos[:1].to(kind).cuda().expand(3, S, n)):
+        at = p.cpu()[torch.tensor(axes)].permute(1, 2, 0)
+        for a in (axes, tuple(axes), bytes(axes), np.array(axes)):
+            q, k = M.qk_norm_rope(x[:, :, :hq], x[:, :, hq: hq + hkv], p, inv.cuda(), axes=a)
+            check(q, exact(qkv[:, :, :hq], at, inv, None, False), dt)
+            check(k.transpose(1, 2), exact(qkv[:, :, hq: hq + hkv], at, inv, None, False), dt)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_equal_axes_are_one(interleaved):
+    """Axes that agree give what one axis gives, bit for bit; in place, too."""
+    qkv, pos, inv, w = case(2, 600, 8, 2, torch.bfloat16, 64, 1, 62)
+    x, p = qkv.cuda(), pos[0].to(torch.int32).cuda()
+    args = (inv.cuda(), w[0].cuda(), w[1].cuda())
+    one = M.qk_norm_rope(x[:, :, :8], x[:, :, 8:10], p, *args, interleaved=interleaved)
+    same = M.qk_norm_rope(x[:, :, :8], x[:, :, 8:10], p.expand(5, 2, 600), *args, interleaved=interleaved, axes=[i % 5 for i in range(32)])
+    assert torch.equal(one[0], same[0]) and torch.equal(one[1], same[1])
+    q, k = x[:, :, :8], x[:, :, 8:10]
+    M.qk_norm_rope(q, k, p.expand(5, 2, 600), *args, interleaved=interleaved, axes=bytes(32), q_out=q, k_out=k.transpose(1, 2))
+    assert torch.equal(q, one[0]) and torch.equal(k.transpose(1, 2), one[1])
+
+
+def test_refusals():
+    qkv, pos, inv, _ = case(2, 3, 4, 2, torch.float16, 128, 3, 63)
+    q, k, p, inv = qkv.cuda()[:, :, :4], qkv.cuda()[:, :, 4:6], pos.to(torch.int32).cuda(), inv.cuda()
+    ok = [i % 3 for i in range(64)]
+    M.qk_norm_rope(q, k, p, inv, axes=ok)
+    for pp, axes in ((p, ok[:63]), (p, ok + [0]), (p, [3] * 64), (p, [-1] * 64), (p, [256] * 64), (p, []), (p[0], ok), (p[:, :1], ok), (p[:0], ok),
+                     (p.long().float(), ok), (p.cpu(), ok), (p, None)):
+        with pytest.raises(ValueError):
+            M.qk_norm_rope(q, k, pp, inv, axes=axes)
