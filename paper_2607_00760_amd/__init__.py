@@ -464,8 +464,8 @@ def qk_norm_rope(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps: f
         if positions.dim() != 3 or not 1 <= positions.shape[0] <= 255:
             raise ValueError(f"positions: shape {tuple(positions.shape)}, expected (axes, {S}, {n}) with 1 to 255 axes")
         axes = bytes(axes) if isinstance(axes, (bytes, tuple, list)) else bytes(int(i) for i in axes)
-        if len(axes) != half or (half and max(axes) >= positions.shape[0]):
-            raise ValueError(f"axes: {len(axes)} of values up to {max(axes, default=0)}, expected {half} below {positions.shape[0]}")
+        if len(axes) != half:
+            raise ValueError(f"axes: {len(axes)} of them, expected {half}")
         call, last = load().mosaic_qk_norm_rope_axes, (positions.shape[0], axes)
     qw = kw = None
     if q_weight is not None:
