@@ -10,7 +10,8 @@
 // softmax with running maximum and sum, O^T += V^T P^T.  With that side of the
 // products a row's logits lie in two lanes, and, the tokens dealt to the first
 // product's rows as the second one asks for them, its weights go into the
-// second product without leaving their lanes.
+// second product without leaving their lanes, rounded to the element type: each
+// is off by half a step at most, as much as the output's own rounding.
 //
 // Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
 // out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
@@ -50,6 +51,16 @@ template <typename F> __device__ __forceinline__ float halves(float x, F f) {
     const uint32_t u = __float_as_uint(x);
     const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     return f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// s and both numbers of a pair
+template <int DT> __device__ __forceinline__ float add2(uint32_t w, float s) {
+    if constexpr (DT) {
+        typedef __attribute__((ext_vector_type(2))) __bf16 b2;
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w), __builtin_bit_cast(b2, 0x3f803f80u), s, false);
+    } else {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(ch2, w), __builtin_bit_cast(ch2, 0x3c003c00u), s, false);
+    }
 }
 
 // Eight numbers in the order in which an operand holds them: as they are in
@@ -342,12 +353,11 @@ template <int DT> struct Rows {
         for (int e = 0; e < 4; ++e) {
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(fmaf(z[e >> 1][8 * (e & 1) + i], zs, mz));
-                l_run += x[i];
-            }
+            for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(fmaf(z[e >> 1][8 * (e & 1) + i], zs, mz));
             pf[e] = make_uint4(pack16<DT>(x[deal<DT>(0)], x[deal<DT>(1)]), pack16<DT>(x[deal<DT>(2)], x[deal<DT>(3)]),
                                pack16<DT>(x[deal<DT>(4)], x[deal<DT>(5)]), pack16<DT>(x[deal<DT>(6)], x[deal<DT>(7)]));
+            // (the sum of the weights as they are rounded: a token that has nearly all keeps its value)
+            l_run = add2<DT>(pf[e].w, add2<DT>(pf[e].z, add2<DT>(pf[e].y, add2<DT>(pf[e].x, l_run))));
         }
     }
 };
