@@ -93,8 +93,9 @@ __global__ void __launch_bounds__(256) k_norm_rope(NormRope a, int rounds) {
                 src = p.in + s * p.in_seq + j * p.in_tok + h * p.in_head;
                 to[it] = p.out + s * p.out_seq + j * p.out_tok + h * p.out_head;
             }
-            x[it][0] = *(const uint2 *)(src + c0);
-            x[it][1] = *(const uint2 *)(src + c1);
+            // (streamed: 32768 tokens of 32 rows, three axes 143 us, 149 without; of 48 rows, one axis 131.5, 133)
+            x[it][0] = __builtin_bit_cast(uint2, __builtin_nontemporal_load((const uint64_t *)(src + c0)));
+            x[it][1] = __builtin_bit_cast(uint2, __builtin_nontemporal_load((const uint64_t *)(src + c1)));
         }
     }
     if (tid < half) {

@@ -24,6 +24,8 @@ namespace {
 
 constexpr int QN4_ARRIVE = 32;
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
 // 16-bit floating patterns as integers of the same order (and back), two in a word
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 __device__ __forceinline__ s16x2 ordered(uint32_t w) {
@@ -124,7 +126,10 @@ __global__ void __launch_bounds__(8 * B) k_quant4_append(Q4Cache q, QNew nw) {
         if (j * B >= f) {                                  // new tokens only
             const uint16_t *row = src + (int64_t)(j * B - f + t0) * tok + 8 * pc;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) { x[r] = *(const uint4 *)row; row += step * tok; }
+            for (int r = 0; r < 4; ++r) {                      // (streamed: 4 x 32785 tokens of 8 heads 257 us, 275 without)
+                x[r] = __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4 *)row));
+                row += step * tok;
+            }
         } else {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
