@@ -640,7 +640,7 @@ mosaic_status mosaic_nibble_workspace_bytes(const mosaic_nibble_cache *cache, si
  * A sequence without tokens gets zeros.  V may be of any magnitude, q and K as
  * long as a head's products of q with scales and zeros, and their sums times
  * sm_scale, stay within fp32; softmax weights below 2^-126 of a head's largest
- * count as zero. */
+ * count as zero.  sm_scale: any finite number. */
 mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *cache, const void *q, float *out, float sm_scale,
                                              void *ws, size_t ws_bytes, void *stream);
 
@@ -656,8 +656,9 @@ mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *cache, c
  *            from new_lens[s] on are neither read nor written; out's rows do not
  *            overlap, out may be q (same pointer and strides)
  *   ws     : at least mosaic_nibble_workspace_bytes bytes, 256-byte aligned
- * Softmax weights are rounded to the dtype before their product with V.  A query
- * that attends nothing gets zeros.  q, K and V as long as a head's products and
+ * Softmax weights are rounded to the dtype before their product with V (below
+ * 2^-35 of a row's largest in fp16, 2^-126 in bf16, they count as zero).
+ * sm_scale: any finite number.  A query that attends nothing gets zeros.  q, K and V as long as a head's products and
  * the sums of weights times values stay within fp32.
  * Errors: INVALID, UNSUPPORTED (head_dim, block_len, max_new past 2^27 or 2^23
  * tiles of 32 rows). */

@@ -13,6 +13,13 @@
 // second product without leaving their lanes, rounded to the element type: each
 // is off by half a step at most, as much as the output's own rounding.
 //
+// What bounds it.  Many rows: 2048 queries of 32 heads over 32 K tokens (8 kv
+// heads, 1.07 TFLOP, causal) take 1000 us, 1.06 PFLOP/s; a bf16 product of 8192^3
+// reaches 1.25.  The matrix unit is busy 55 % of the cycles, at 1.9 GHz of 2.4: the
+// card's power holds the clock down, and codes are worked out and weights made
+// meanwhile.  Few rows: 5 queries over 8 x 32 K tokens take 92 us, 3.2 TB/s: a
+// wave's codes, logits, weights and outputs are one chain, two waves a SIMD.
+//
 // Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
 // out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
 // wave takes 64 tokens of its own, keys and values one after the other in LDS of
@@ -27,7 +34,7 @@ namespace mosaic {
 namespace {
 
 constexpr int CK_TILE = 64;                                // tokens of a step
-constexpr int CK_SLOTS = 256;                              // workgroups that take part in splits, at most
+constexpr int CK_SLOTS = 256;                              // workgroups that take part in splits, at most (one a compute unit)
 constexpr int CK_ROWS = 256;                               // rows of a workgroup at most
 constexpr int CK_FEW = 32, CK_FEW_WAVES = 8;
 
@@ -158,8 +165,9 @@ template <int B, int DT, int GT, bool VALS> struct Step {
     }
     // Codes and grids of step t; of one whose blocks are not whole, zeros.  (Through
     // buffer descriptors: a step is scalar work, and there is no branch, at whose end
-    // the compiler would wait for what was loaded.  2048 queries 1124 us with the
-    // addresses in vector registers, 898 without loads.)
+    // the compiler would wait for what was loaded.  2048 queries over 32 K tokens
+    // 1047 us with addresses in vector registers and the step's kind asked in the
+    // loop, 1005 so.)
     __device__ __forceinline__ void load(const Q4Cache &q, uint64_t pb, int whole, int t, int gt) {
         const bool live = NB * (t + 1) <= whole;
         const uint64_t blk = pb + (live ? (uint32_t)(NB * t) : 0u);
@@ -583,7 +591,13 @@ hipError_t launch_quant4_chunk(const Q4Cache &q, int block, int dtype, const QCh
     const int pairs = q.S * q.H, all = c.n * q.G;
     const int rows = all <= CK_FEW ? CK_FEW : (all <= 128 ? 128 : CK_ROWS), tiles = (all + rows - 1) / rows;
     const long long wgs = (long long)pairs * tiles;
-    // a split has a step for each wave (of few rows) or four at least
+    // us of 6 x 1500 tokens, 448 rows, 72 pairs: 128 rows a workgroup 60.2, 256 49.8; 1 x 8 K, 256 rows, 8 pairs, best
+    // splits: 128 34.2, 256 36.6; 4 x 4 K, 400 rows, 32 pairs: 128 55.4, 256 50.7.  32 rows alone go to k_chunk_few.
+    // More workgroups than compute units run one after the other, and their parts are memory traffic: 6 x 1500 tokens
+    // 49.8 with one workgroup a tile (144), 73.6 with two; 2 x 16 K, 1200 rows (80 tiles): 404 / 176 / 247 with one,
+    // three and four.  Up to a workgroup a compute unit splits pay: 1 x 2 K, 2048 rows (64 tiles) 58.2 / 36.7 / 52.5 with
+    // one, four and eight; few rows, 1 x 32 K, 8 pairs: 43.6 / 32.6 / 52.4 with 8, 32 and 64, and 1 x 2 K 21.8 / 14.6 with
+    // one and four.  A split has a step for each wave (of few rows) or four at least.
     const int most = ceil_div(q.cap, (rows == CK_FEW ? CK_FEW_WAVES : 4) * CK_TILE);
     int ns = (int)(CK_SLOTS / wgs);
     ns = ns < 1 ? 1 : (ns > most ? most : ns);

@@ -1,6 +1,7 @@
 // quant_api.hip -- C ABI of the operators around the 8-bit and the 4-bit KV
 // cache and of the norm-and-rotation pass (see include/mosaic.h): argument validation,
 // workspace layout, launches.  No C++ exception crosses the ABI.
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 
@@ -333,6 +334,7 @@ mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *c, const
     if (st != MOSAIC_OK) return st;
     if (!q || !out || !ws) return fail(MOSAIC_ERR_INVALID, "NULL argument");
     if (off16(q) || off16(out)) return fail(MOSAIC_ERR_INVALID, "q and out must be 16-byte aligned");
+    if (!std::isfinite(sm_scale)) return fail(MOSAIC_ERR_INVALID, "sm_scale not finite");
     const mosaic_status sw = quant4_ws_args(c, ws, ws_bytes);
     if (sw != MOSAIC_OK) return sw;
     return done(launch_quant4_attn(qc, c->block_len, c->dtype, (const uint16_t *)q, sm_scale, ws, out, (hipStream_t)stream), "attention launch");
@@ -351,6 +353,7 @@ mosaic_status mosaic_nibble_attend(const mosaic_nibble_cache *c, const void *q, 
         return fail(MOSAIC_ERR_INVALID, "q/out must be 16-byte aligned, their strides multiples of 8 elements");
     if (rows_overlap(out_strides, S, max_new, heads)) return fail(MOSAIC_ERR_INVALID, "rows of an output overlap");
     if ((uintptr_t)new_lens % 4) return fail(MOSAIC_ERR_INVALID, "new_lens must be 4-byte aligned");
+    if (!std::isfinite(sm_scale)) return fail(MOSAIC_ERR_INVALID, "sm_scale not finite");
     const mosaic_status sw = quant4_ws_args(c, ws, ws_bytes);
     if (sw != MOSAIC_OK) return sw;
     if (max_new == 0) return done(hipSuccess, "");

@@ -31,12 +31,13 @@ def read(lib, c, k=FAKE, v=FAKE, ks=three(8192, 1024, 128), vs=three(8192, 1024,
     return call(C.byref(c), k, v, ks, vs, starts, start, n, None)
 
 
-def decode(lib, c, q=FAKE, out=FAKE, ws=FAKE, nbytes=1 << 40):
-    return lib.mosaic_nibble_decode_attention(C.byref(c), q, out, C.c_float(0.1), ws, nbytes, None)
+def decode(lib, c, q=FAKE, out=FAKE, ws=FAKE, nbytes=1 << 40, scale=0.1):
+    return lib.mosaic_nibble_decode_attention(C.byref(c), q, out, C.c_float(scale), ws, nbytes, None)
 
 
-def attend(lib, c, q=FAKE, out=FAKE, qs=three(32768, 4096, 128), os=three(32768, 4096, 128), lens=None, n=8, ws=FAKE, nbytes=1 << 40):
-    return lib.mosaic_nibble_attend(C.byref(c), q, out, qs, os, lens, n, 1, C.c_float(0.1), ws, nbytes, None)
+def attend(lib, c, q=FAKE, out=FAKE, qs=three(32768, 4096, 128), os=three(32768, 4096, 128), lens=None, n=8, ws=FAKE, nbytes=1 << 40,
+           scale=0.1):
+    return lib.mosaic_nibble_attend(C.byref(c), q, out, qs, os, lens, n, 1, C.c_float(scale), ws, nbytes, None)
 
 
 def rope(lib, **kw):
@@ -87,7 +88,8 @@ def test_arguments_that_are_refused(lib):  # noqa: F811
             assert read(lib, what, start=start, n=(1 << 31) - 1) == OK and lib.fake_calls() == 1
     refused(lib, CAPACITY, lambda: append(lib, c, n=6401))
     refused(lib, UNSUPPORTED, lambda: append(lib, c, n=1 << 28, lens=FAKE))
-    for kw in (dict(q=None), dict(out=None), dict(ws=None), dict(q=FAKE + 8), dict(out=FAKE + 8), dict(ws=FAKE + 16), dict(nbytes=n.value - 1)):
+    for kw in (dict(q=None), dict(out=None), dict(ws=None), dict(q=FAKE + 8), dict(out=FAKE + 8), dict(ws=FAKE + 16), dict(nbytes=n.value - 1),
+               dict(scale=float("inf")), dict(scale=float("nan"))):
         refused(lib, INVALID, lambda: decode(lib, c, **kw))
         refused(lib, INVALID, lambda: attend(lib, c, **kw))
     for kw in (dict(qs=None), dict(os=None), dict(qs=three(32768, 4092, 128)), dict(os=three(32768, 4096, 4)), dict(os=three(32768, 4096, 64)),
