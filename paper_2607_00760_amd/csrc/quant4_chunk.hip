@@ -37,6 +37,7 @@ constexpr int CK_TILE = 64;                                // tokens of a step
 constexpr int CK_SLOTS = 256;                              // workgroups that take part in splits, at most (one a compute unit)
 constexpr int CK_ROWS = 256;                               // rows of a workgroup at most
 constexpr int CK_FEW = 32, CK_FEW_WAVES = 8;
+constexpr int CK_LEAST = 4;                                // steps of a share at least (of few rows: one for each wave)
 
 // Weights of fp16 are this power of two times as large: those of 2^-25 and less
 // of the row's largest would vanish, and a million of them count.  The running
@@ -125,12 +126,13 @@ template <> struct Grid8<0> {
     }
 };
 
-// a row tile's share of the work, the same in the attention and in the join
+// a row tile, and the workgroup's share of it
 struct ChunkPlan {
     int p, s, h, row0;                                     // pair, its sequence and kv head, the tile's first row
-    int L, m, nt, per, used;                               // tokens, queries, steps of 64, of a split, splits with any
+    int L, m, nt;                                          // tokens, queries, steps of 64 (-1: no rows)
+    int t0, t1;                                            // the share's steps
 };
-__device__ __forceinline__ ChunkPlan chunk_plan(const Q4Cache &q, const QChunk &c, int id, int tiles, int rows, int ns) {
+__device__ __forceinline__ ChunkPlan chunk_tile(const Q4Cache &q, const QChunk &c, int id, int tiles, int rows) {
     ChunkPlan r;
     const int pairs = q.S * q.H, t = tiles - 1 - id / pairs;       // (a pair's last tiles see most: first; one XCD's, if H is 8)
     r.p = id % pairs;
@@ -140,10 +142,99 @@ __device__ __forceinline__ ChunkPlan chunk_plan(const Q4Cache &q, const QChunk &
     r.L = q.len(r.p);
     r.m = min(max(c.counts ? c.counts[r.s] : c.n, 0), c.n);
     const int last = min(r.m - 1, (r.row0 + rows - 1) / q.G);      // the tile's last query
-    const int seen = r.row0 >= r.m * q.G ? 0 : max(c.causal ? r.L - r.m + last + 1 : r.L, 0);
-    r.nt = (seen + CK_TILE - 1) / CK_TILE;
-    r.per = (r.nt + ns - 1) / ns;
-    r.used = r.per ? (r.nt + r.per - 1) / r.per : 0;
+    r.nt = r.row0 >= r.m * q.G ? -1 : (max(c.causal ? r.L - r.m + last + 1 : r.L, 0) + CK_TILE - 1) / CK_TILE;
+    r.t0 = 0;
+    r.t1 = r.nt;
+    return r;
+}
+
+// Fewer tiles than CK_SLOTS: workgroups are dealt to them by their steps, as few
+// for one as keep all shares of `per` steps (a multiple of STEP, at least LEAST)
+// within CK_SLOTS.  Lengths are read on the device, so a captured launch follows
+// them.  What workgroup w belongs to; one wave works it out, a lane holds up to
+// four tiles in a row.
+// (behind the shares' results: a tile's first workgroup, and how many it has)
+__device__ __forceinline__ int2 *chunk_table(float *part) { return (int2 *)(part + (uint64_t)CK_SLOTS * CK_ROWS * (D + 4)); }
+struct ChunkShare { int id, first, used, per; };           // tile (-1: none), its first workgroup, how many, steps of each
+template <int STEP, int LEAST> __device__ __forceinline__ ChunkShare chunk_share(const Q4Cache &q, const QChunk &c, int tiles, int rows, int w) {
+    const int units = q.S * q.H * tiles, lane = threadIdx.x & 63, K = (units + 63) / 64;
+    int g[4] = {-1, -1, -1, -1};                           // steps in STEPs
+    uint32_t sum = 0, most = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int id = K * lane + j;
+        if (j < K && id < units) {
+            const int nt = chunk_tile(q, c, id, tiles, rows).nt;
+            g[j] = nt < 0 ? -1 : (nt + STEP - 1) / STEP;
+            sum += (uint32_t)min(max(g[j], 0), 1 << 23);
+            most = max(most, (uint32_t)max(g[j], 0));
+        }
+    }
+    sum = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(sum), 63);
+    // g[j] / per rounded up, 1 at least (fp32's quotient is off by one at most)
+    auto shares = [&](int j, uint32_t per) {
+        const uint32_t y = (uint32_t)g[j] + per - 1u, k = (uint32_t)((float)y * __builtin_amdgcn_rcpf((float)per));
+        const int rest = (int)(y - k * per);
+        return g[j] < 0 ? 0u : max(1u, rest < 0 ? k - 1u : (rest >= (int)per ? k + 1u : k));
+    };
+    auto upto = [&](uint32_t per) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < K) n += shares(j, per);
+        return wave_scan_add(n);
+    };
+    auto fits = [&](uint32_t per) { return __builtin_amdgcn_readlane((int)upto(per), 63) <= CK_SLOTS; };
+    uint32_t per = max((uint32_t)(LEAST / STEP), (sum + CK_SLOTS - 1) / CK_SLOTS);
+    if (!fits(per)) {
+        for (int o = 32; o; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+        uint32_t no = per;
+        per = (uint32_t)__builtin_amdgcn_readfirstlane((int)most);         // (one workgroup a tile)
+        while (per - no > 1) {
+            const uint32_t mid = (per + no) / 2;
+            if (fits(mid)) per = mid; else no = mid;
+        }
+    }
+    int first = (int)upto(per), id = -1, f = 0, used = 0;
+#pragma unroll
+    for (int j = 3; j >= 0; --j) {
+        const int n = (int)shares(j, per);
+        first -= n;
+        if (w >= first && w < first + n) { id = K * lane + j; f = first; used = n; }
+    }
+    const uint64_t here = __ballot(id >= 0);
+    if (here == 0) return ChunkShare{-1, 0, 0, 0};
+    const int src = __builtin_ctzll(here);
+    return ChunkShare{__builtin_amdgcn_readlane(id, src), __builtin_amdgcn_readlane(f, src), __builtin_amdgcn_readlane(used, src), (int)per * STEP};
+}
+__device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
+// steps of each of a tile's ns shares
+__device__ __forceinline__ int even_share(int nt, int ns, int step) { return max(div_up(div_up(nt, step), ns), 1) * step; }
+// The workgroup's plan; used: how many workgroups its tile has (0: nothing to do).
+// shared > 0: every tile has so many; < 0: they are dealt by the tiles' steps, and
+// the first of a tile writes (first, used) to `table` for the join.
+template <int STEP, int LEAST>
+__device__ __forceinline__ ChunkPlan chunk_plan(const Q4Cache &q, const QChunk &c, int tiles, int rows, int shared, int2 *table, int &used) {
+    __shared__ ChunkShare sh;
+    if (shared < 0) {
+        if (threadIdx.x < 64) {
+            const ChunkShare x = chunk_share<STEP, LEAST>(q, c, tiles, rows, blockIdx.x);
+            if (threadIdx.x == 0) {
+                sh = x;
+                if (x.id >= 0 && x.first == (int)blockIdx.x) table[x.id] = make_int2(x.first, x.used);
+            }
+        }
+        __syncthreads();
+    }
+    const int ns = max(shared, 1), id = shared < 0 ? __builtin_amdgcn_readfirstlane(sh.id) : (int)blockIdx.x / ns;
+    ChunkPlan r = chunk_tile(q, c, max(id, 0), tiles, rows);
+    used = id < 0 || r.nt < 0 ? 0 : 1;
+    if (shared && used) {
+        const int per = shared < 0 ? __builtin_amdgcn_readfirstlane(sh.per) : even_share(r.nt, ns, STEP);
+        r.t0 = ((int)blockIdx.x - (shared < 0 ? __builtin_amdgcn_readfirstlane(sh.first) : id * ns)) * per;
+        r.t1 = min(r.nt, r.t0 + per);
+        used = shared < 0 ? __builtin_amdgcn_readfirstlane(sh.used) : (r.t0 && r.t0 >= r.t1 ? 0 : div_up(max(r.nt, 1), per));
+    }
     return r;
 }
 
@@ -377,18 +468,17 @@ __device__ __forceinline__ uint16_t *out_row(const Q4Cache &q, const QChunk &c, 
 }
 __device__ __forceinline__ float power_of(float m, float zs) { return m == -INFINITY ? m : m * zs; }
 
-// grid (row tiles, splits and pairs); RW waves of 32 rows
+// grid (row tiles and pairs), or (shares of them) where `shared` is not 0; RW waves of 32 rows
 template <int B, int DT, int RW>
 __global__ void __launch_bounds__(64 * RW) __attribute__((amdgpu_waves_per_eu(2)))
-k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
+k_chunk(Q4Cache q, QChunk c, int tiles, int shared, float *part) {
     constexpr int KB = CK_TILE * D * 2;                    // bytes of a step's keys, and of its values
     __shared__ __align__(16) uint8_t kl[2][KB], vl[2][KB];
-    const int id = blockIdx.x / ns, split = blockIdx.x - id * ns;
-    const ChunkPlan pl = chunk_plan(q, c, id, tiles, 32 * RW, ns);
-    if (pl.row0 >= pl.m * q.G) return;
+    int used;
+    const ChunkPlan pl = chunk_plan<1, CK_LEAST>(q, c, tiles, 32 * RW, shared, chunk_table(part), used);
+    if (used == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int t0 = split * pl.per, t1 = min(pl.nt, t0 + pl.per);
-    if (split > 0 && t0 >= t1) return;                     // (split 0 writes what nothing is seen of, too)
+    const int t0 = pl.t0, t1 = pl.t1;
     const int hl = lane >> 5, row = pl.row0 + 32 * wave + (lane & 31);
     const int all = c.causal ? pl.L - pl.m + pl.row0 / q.G + 1 : pl.L;     // tokens that every row of the workgroup attends
     const int whole = pl.L / B, tail = pl.L % B;
@@ -448,7 +538,7 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
         else work(std::false_type{});
     }
     const float l = halves(r.l_run, [](float a, float b) { return a + b; }), inv = share_of(l);
-    if (pl.used <= 1) {
+    if (used == 1) {
         if (!r.valid) return;
         uint16_t *op = out_row(q, c, pl, row) + 4 * hl;
 #pragma unroll
@@ -459,7 +549,7 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
                                                               pack16<DT>(r.acc[ct][4 * a + 2] * inv, r.acc[ct][4 * a + 3] * inv));
         return;
     }
-    // a split's averages, and (maximum, sum)
+    // a share's averages, and (maximum, sum)
     float *to = part + ((uint64_t)blockIdx.x * (32 * RW) + (row - pl.row0)) * (D + 4);
     if (hl == 0) *(float2 *)to = make_float2(power_of(r.m_run, r.zs), l);
 #pragma unroll
@@ -470,19 +560,18 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int ns, float *part) {
                                                                          r.acc[ct][4 * a + 2] * inv, r.acc[ct][4 * a + 3] * inv);
 }
 
-// at most 32 rows: grid (splits and pairs)
+// at most 32 rows: grid (pairs), or (shares of them)
 template <int B, int DT>
 __global__ void __launch_bounds__(64 * CK_FEW_WAVES) __attribute__((amdgpu_waves_per_eu(2)))
-k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
+k_chunk_few(Q4Cache q, QChunk c, int shared, float *part) {
     constexpr int W = CK_FEW_WAVES, KB = CK_TILE * D * 2;
     __shared__ __align__(16) uint8_t lds[W][KB];
     __shared__ float ml[W][32][2];
-    const int id = blockIdx.x / ns, split = blockIdx.x - id * ns;
-    const ChunkPlan pl = chunk_plan(q, c, id, 1, CK_FEW, ns);
-    if (pl.m == 0) return;
+    int used;
+    const ChunkPlan pl = chunk_plan<W, W>(q, c, 1, CK_FEW, shared, chunk_table(part), used);
+    if (used == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int t0 = split * pl.per, t1 = min(pl.nt, t0 + pl.per);
-    if (split > 0 && t0 >= t1) return;                     // (split 0 writes what nothing is seen of, too)
+    const int t0 = pl.t0, t1 = pl.t1;
     const int l32 = lane & 31, hl = lane >> 5;
     const int all = c.causal ? pl.L - pl.m + 1 : pl.L;     // tokens that every row attends
     const int whole = pl.L / B, tail = pl.L % B;
@@ -544,7 +633,7 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
         for (int w = 0; w < W; ++w) x[i] += f[w] * ((const float *)lds[w])[(16 * wave + 8 * hl + i) * 32 + l32];
         x[i] *= inv;
     }
-    if (pl.used <= 1) {
+    if (used == 1) {
         if (r.valid)
             *(uint4 *)(out_row(q, c, pl, l32) + 16 * wave + 8 * hl) = make_uint4(pack16<DT>(x[0], x[1]), pack16<DT>(x[2], x[3]), pack16<DT>(x[4], x[5]),
                                                                                  pack16<DT>(x[6], x[7]));
@@ -556,18 +645,21 @@ k_chunk_few(Q4Cache q, QChunk c, int ns, float *part) {
     *(float4 *)(to + 8 + 16 * wave + 8 * hl) = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-// the splits of a row tile joined, in their order; grid (row tiles and pairs, rows / 8), 32 lanes a row
+// the shares of a row tile joined, in their order; grid (row tiles and pairs, rows / 8), 32 lanes a row
 template <int DT>
-__global__ void __launch_bounds__(256) k_chunk_join(Q4Cache q, QChunk c, int tiles, int rows, int ns, const float *part) {
-    const ChunkPlan pl = chunk_plan(q, c, blockIdx.x, tiles, rows, ns);
-    if (pl.used <= 1) return;
+__global__ void __launch_bounds__(256) k_chunk_join(Q4Cache q, QChunk c, int tiles, int rows, int shared, float *part) {
+    const ChunkPlan pl = chunk_tile(q, c, blockIdx.x, tiles, rows);
+    // (a tile without rows has no entry, and writes nothing)
+    const int2 sh = shared < 0 ? chunk_table(part)[blockIdx.x]
+                               : make_int2((int)blockIdx.x * shared, div_up(max(pl.nt, 1), even_share(pl.nt, shared, rows == CK_FEW ? CK_FEW_WAVES : 1)));
+    if (sh.y <= 1) return;
     const int r = 8 * blockIdx.y + (threadIdx.x >> 5), ch = 4 * (threadIdx.x & 31);
     const int row = pl.row0 + r, qi = row / q.G, head = pl.h * q.G + row - qi * q.G;
     if (qi >= pl.m) return;
-    const float *from = part + (uint64_t)blockIdx.x * ns * rows * (D + 4) + r * (D + 4);
+    const float *from = part + (uint64_t)sh.x * rows * (D + 4) + r * (D + 4);
     float M = -INFINITY, S = 0.0f;
     float4 A = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int k = 0; k < pl.used; ++k) {
+    for (int k = 0; k < sh.y; ++k) {
         const float *o = from + (uint64_t)k * rows * (D + 4);
         const float2 x = *(const float2 *)o;
         const float4 a = *(const float4 *)(o + 4 + ch);
@@ -585,7 +677,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(Q4Cache q, QChunk c, int til
 
 }  // namespace
 
-size_t quant4_chunk_ws_bytes() { return (size_t)CK_SLOTS * CK_ROWS * (D + 4) * sizeof(float); }
+size_t quant4_chunk_ws_bytes() { return (size_t)CK_SLOTS * (CK_ROWS * (D + 4) * sizeof(float) + sizeof(int2)); }
 
 hipError_t launch_quant4_chunk(const Q4Cache &q, int block, int dtype, const QChunk &c, float *part, hipStream_t s) {
     const int pairs = q.S * q.H, all = c.n * q.G;
@@ -593,28 +685,30 @@ hipError_t launch_quant4_chunk(const Q4Cache &q, int block, int dtype, const QCh
     const long long wgs = (long long)pairs * tiles;
     // us of 6 x 1500 tokens, 448 rows, 72 pairs: 128 rows a workgroup 60.2, 256 49.8; 1 x 8 K, 256 rows, 8 pairs, best
     // splits: 128 34.2, 256 36.6; 4 x 4 K, 400 rows, 32 pairs: 128 55.4, 256 50.7.  32 rows alone go to k_chunk_few.
-    // More workgroups than compute units run one after the other, and their parts are memory traffic: 6 x 1500 tokens
-    // 49.8 with one workgroup a tile (144), 73.6 with two; 2 x 16 K, 1200 rows (80 tiles): 404 / 176 / 247 with one,
-    // three and four.  Up to a workgroup a compute unit splits pay: 1 x 2 K, 2048 rows (64 tiles) 58.2 / 36.7 / 52.5 with
-    // one, four and eight; few rows, 1 x 32 K, 8 pairs: 43.6 / 32.6 / 52.4 with 8, 32 and 64, and 1 x 2 K 21.8 / 14.6 with
-    // one and four.  A split has a step for each wave (of few rows) or four at least.
-    const int most = ceil_div(q.cap, (rows == CK_FEW ? CK_FEW_WAVES : 4) * CK_TILE);
-    int ns = (int)(CK_SLOTS / wgs);
-    ns = ns < 1 ? 1 : (ns > most ? most : ns);
-    const dim3 grid((uint32_t)(wgs * ns));
+    // More workgroups than compute units run one after the other, and their parts are memory traffic (6 x 1500 tokens,
+    // 144 tiles, 49.8 with one workgroup each, 73.6 with two), so tiles are shared among as many as there are units.
+    // A sequence alone: evenly (1 x 2 K, 2048 rows, 64 tiles, 58.2 / 36.7 / 52.5 with one, four and eight a tile).  Several:
+    // by their steps, as they may differ.  Evenly / by steps, ragged batches: 6 x up to 1500 tokens 50.2 / 45.2, 5 queries
+    // over 8 x up to 32 K 74 / 56, over 16 x up to 8 K 43.0 / 38.2; batches of one length pay for the dealing, 5 over 8 x 32 K
+    // 84.5 / 84, 100 over 4 x 4 K 49.7 / 50.4, 5 over 24 x 8 K (192 tiles, not shared, not joined) 69.5 / 73.3, 6 x 1500 51 / 57.
+    const int least = rows == CK_FEW ? CK_FEW_WAVES : CK_LEAST, most = ceil_div(ceil_div(q.N, CK_TILE / block), least);
+    const int ns = wgs < CK_SLOTS ? (most < CK_SLOTS / (int)wgs ? most : CK_SLOTS / (int)wgs) : 1;
+    const int shared = wgs >= CK_SLOTS || most == 1 || (q.S == 1 && ns == 1) ? 0 : (q.S == 1 ? ns : -1);
+    const long long all_shares = shared < 0 ? wgs * most : wgs * ns;
+    const dim3 grid((uint32_t)(shared < 0 && all_shares > CK_SLOTS ? CK_SLOTS : all_shares));
     auto by_rows = [&](auto b, auto dt) {
         constexpr int BL = decltype(b)::value, T = decltype(dt)::value;
-        if (rows == CK_FEW) hipLaunchKernelGGL((k_chunk_few<BL, T>), grid, dim3(64 * CK_FEW_WAVES), 0, s, q, c, ns, part);
-        else if (rows == 128) hipLaunchKernelGGL((k_chunk<BL, T, 4>), grid, dim3(256), 0, s, q, c, tiles, ns, part);
-        else hipLaunchKernelGGL((k_chunk<BL, T, 8>), grid, dim3(512), 0, s, q, c, tiles, ns, part);
+        if (rows == CK_FEW) hipLaunchKernelGGL((k_chunk_few<BL, T>), grid, dim3(64 * CK_FEW_WAVES), 0, s, q, c, shared, part);
+        else if (rows == 128) hipLaunchKernelGGL((k_chunk<BL, T, 4>), grid, dim3(256), 0, s, q, c, tiles, shared, part);
+        else hipLaunchKernelGGL((k_chunk<BL, T, 8>), grid, dim3(512), 0, s, q, c, tiles, shared, part);
     };
     auto by_type = [&](auto b) { if (dtype) by_rows(b, std::integral_constant<int, 1>{}); else by_rows(b, std::integral_constant<int, 0>{}); };
     if (block == 32) by_type(std::integral_constant<int, 32>{}); else by_type(std::integral_constant<int, 64>{});
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || ns == 1) return e;
+    if (e != hipSuccess || !shared) return e;
     const dim3 jgrid((uint32_t)wgs, rows / 8);
-    if (dtype) hipLaunchKernelGGL(k_chunk_join<1>, jgrid, dim3(256), 0, s, q, c, tiles, rows, ns, part);
-    else hipLaunchKernelGGL(k_chunk_join<0>, jgrid, dim3(256), 0, s, q, c, tiles, rows, ns, part);
+    if (dtype) hipLaunchKernelGGL(k_chunk_join<1>, jgrid, dim3(256), 0, s, q, c, tiles, rows, shared, part);
+    else hipLaunchKernelGGL(k_chunk_join<0>, jgrid, dim3(256), 0, s, q, c, tiles, rows, shared, part);
     return hipGetLastError();
 }
 
