@@ -36,14 +36,14 @@ struct QNew {                                              // tokens to append, 
 
 // How a launch shares the units of all pairs: in runs of c units that do not
 // cross pairs, c the least that makes about `slots` runs, a multiple of step
-// and at least cmin; from there up to 2 cmin for about `few` runs.  The lengths
+// and at least cmin; from there up to much for about `few` runs.  The lengths
 // are read on the device, so a captured launch follows them; runs are equal
 // however ragged the batch, and there are at most slots + pairs of them.
 struct QShare {
-    int slots, few, cmin, step;
+    int slots, few, cmin, much, step;
     int least;                                             // runs of a pair at least
     int alone;                                             // units that a pair's only run may have, whatever c is
-    int join;                                              // runs that are joined in one go: pairs of up to join * 2 cmin
+    int join;                                              // runs that are joined in one go: pairs of up to join * much
                                                            // units have no more
 };
 struct QPlan {
@@ -62,14 +62,14 @@ __device__ __forceinline__ QPlan q_plan(const C &q, const QShare &sh, U units, i
     for (int s = lane + 64; s < q.S; s += 64) total += (uint32_t)units(length(s));
     total = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_add(total), 63) * (uint32_t)q.H;
     auto runs_of = [&](int n) { return (int)((total + (uint32_t)(n * sh.step) - 1u) / (uint32_t)(n * sh.step)) * sh.step; };
-    const int c = max(max(sh.cmin, min(2 * sh.cmin, runs_of(sh.few))), runs_of(sh.slots));
+    const int c = max(max(sh.cmin, min(sh.much, runs_of(sh.few))), runs_of(sh.slots));
     QPlan p{};
     uint32_t base = 0;
     for (int s0 = 0; s0 < q.S; s0 += 64) {
         const int s = s0 + lane, L = s0 ? length(s) : L0;
         const int u = s < q.S ? units(L) : 0;
         int cu = u <= sh.alone ? max(c, sh.alone) : c;
-        if (u > sh.join * c && u <= sh.join * 2 * sh.cmin) cu = (u + sh.join * sh.step - 1) / (sh.join * sh.step) * sh.step;
+        if (u > sh.join * c && u <= sh.join * sh.much) cu = (u + sh.join * sh.step - 1) / (sh.join * sh.step) * sh.step;
         const int ns = s < q.S ? max(sh.least, (u + cu - 1) / cu) : 0;
         const uint32_t inc = wave_scan_add((uint32_t)(ns * q.H));
         const uint64_t hit = __ballot(base + inc > (uint32_t)w);       // the first sequence whose runs end past w

@@ -41,10 +41,19 @@ namespace mosaic {
 
 namespace {
 
-// as in the 8-bit cache's attention: runs of a launch, units of a run at least, of a pair's only run, of a pair
-// that is joined in one go
+// Runs of a launch, as in the 8-bit cache's attention: they fill the 512 workgroups
+// that the chip holds once.
 __host__ __device__ __forceinline__ int q4_runs(int pairs) { return pairs <= 256 ? 512 - pairs : 1024; }
-constexpr int Q4_LEAST = 2 * QA_NWV, Q4_FEW = 256, Q4_ALONE = 16, Q4_JOIN = 16;
+// Units of a run at least: a step a wave, and up to four rather than a second
+// workgroup on a compute unit.  us of calls, 8 kv heads, blocks of 64, with runs of
+// 4 to 16 units / 8 to 16 / 12 to 24 / 4 to 8:
+//   1 x 1500 tokens      9.0 / 11.1 / 12.8 /  9.0
+//   1 x 4117            10.7 / 10.8 / 12.3 / 10.8
+//   4 x 8192            15.6 / 15.6 / 15.7 / 18.2
+// A pair of up to 512 tokens is one run: 380 (blocks of 32) 8.1, and 9.1 with two;
+// 1000 (blocks of 64) 12.2 as one, 11.1 with two, 8.8 with four.
+constexpr int Q4_LEAST = QA_NWV, Q4_MUCH = 4 * QA_NWV, Q4_FEW = 256, Q4_JOIN = 16;
+template <int B> constexpr int Q4_ALONE = 512 / B;
 
 template <int B> struct Q4Stage {                          // a block in flight
     uint4 k[B / 16];                                       // 32 channels of a token each
@@ -108,7 +117,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
     __shared__ uint4 grids[QA_NWV][(2 * D + 2 * B) / 8];   // a wave's block: scales and zeros of channels, of tokens
     __shared__ int last;
     auto units = [&](int L) { return (L + B - 1) / B; };   // the unfinished block is a pair's last unit
-    const QPlan pl = q_plan(q, QShare{q4_runs(q.S * q.H), Q4_FEW, Q4_LEAST, QA_NWV, 1, Q4_ALONE, Q4_JOIN}, units, blockIdx.x);
+    const QPlan pl = q_plan(q, QShare{q4_runs(q.S * q.H), Q4_FEW, Q4_LEAST, Q4_MUCH, QA_NWV, 1, Q4_ALONE<B>, Q4_JOIN}, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -111,7 +111,7 @@ k_quant_attn(QCache q, QSel sel, const uint16_t *query, float scale, uint32_t *a
     __shared__ int last;
     auto blocks = [&](int L) { return SEL ? q_want(L / B, sel.num, sel.den) : L / B; };
     auto units = [&](int L) { return blocks(L) + (L % B != 0); };        // the unfinished block is a pair's last unit
-    const QPlan pl = q_plan(q, QShare{qa_runs(q.S * q.H), QA_FEW, QA_LEAST, QA_NWV, 1, QA_ALONE, QA_JOIN}, units, blockIdx.x);
+    const QPlan pl = q_plan(q, QShare{qa_runs(q.S * q.H), QA_FEW, QA_LEAST, 2 * QA_LEAST, QA_NWV, 1, QA_ALONE, QA_JOIN}, units, blockIdx.x);
     if (!pl.live) return;
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -108,7 +108,7 @@ __device__ __forceinline__ void score_blocks(const QCache &q, int p, int nb, con
 // grid QS_RUNS + pairs: one run of 64-block units of a pair each
 template <int DT>
 __global__ void __launch_bounds__(256) k_quant_score(QCache q, int block, const uint16_t *query, float *scores, int32_t *list) {
-    const QPlan pl = q_plan(q, QShare{QS_RUNS, QS_RUNS, 1, 1, 0, 0, 0}, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
+    const QPlan pl = q_plan(q, QShare{QS_RUNS, QS_RUNS, 1, 2, 1, 0, 0, 0}, [&](int L) { return (L / block + QS_UNIT - 1) / QS_UNIT; }, blockIdx.x);
     if (!pl.live) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int p = pl.s * q.H + pl.h, nb = pl.L / block;
