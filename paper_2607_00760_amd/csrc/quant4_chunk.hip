@@ -17,14 +17,15 @@
 // heads, 1.07 TFLOP, causal) take 1000 us, 1.06 PFLOP/s; a bf16 product of 8192^3
 // reaches 1.25.  The matrix unit is busy 55 % of the cycles, at 1.9 GHz of 2.4: the
 // card's power holds the clock down, and codes are worked out and weights made
-// meanwhile.  Few rows: 5 queries over 8 x 32 K tokens take 92 us, 3.2 TB/s: a
+// meanwhile.  Few rows: 5 queries over 8 x 32 K tokens take 89 us, 3.3 TB/s: a
 // wave's codes, logits, weights and outputs are one chain, two waves a SIMD.
 //
 // Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
 // out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
 // wave takes 64 tokens of its own, keys and values one after the other in LDS of
 // its own, and they are joined at the end.  Where there are too few rows for the
-// chip the tokens are split over workgroups, which k_chunk_join joins.
+// chip the tokens are shared among workgroups, by the steps that each row tile
+// has, and k_chunk_join joins them.
 #include <type_traits>
 
 #include "quant4.h"
