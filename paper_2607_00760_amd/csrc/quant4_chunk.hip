@@ -14,7 +14,7 @@
 // is off by half a step at most, as much as the output's own rounding.
 //
 // What bounds it.  Many rows: 2048 queries of 32 heads over 32 K tokens (8 kv
-// heads, 1.07 TFLOP, causal) take 1000 us, 1.06 PFLOP/s; a bf16 product of 8192^3
+// heads, 1.07 TFLOP, causal) take 991 to 1044 us, 1.02 to 1.07 PFLOP/s; a bf16 product of 8192^3
 // reaches 1.25.  The matrix unit is busy 55 % of the cycles, at 1.9 GHz of 2.4: the
 // card's power holds the clock down, and codes are worked out and weights made
 // meanwhile.  Few rows: 5 queries over 8 x 32 K tokens take 89 us, 3.3 TB/s: a
