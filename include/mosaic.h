@@ -638,9 +638,9 @@ mosaic_status mosaic_nibble_workspace_bytes(const mosaic_nibble_cache *cache, si
  *   out : [S][H * group_size][128] fp32, 16-byte aligned
  *   ws  : at least mosaic_nibble_workspace_bytes bytes, 256-byte aligned
  * A sequence without tokens gets zeros.  V may be of any magnitude, q and K as
- * long as a head's products of q with scales and zeros, and their sums times
- * sm_scale, stay within fp32; softmax weights below 2^-126 of a head's largest
- * count as zero.  sm_scale: any finite number. */
+ * long as a head's products of q with scales and zeros, their sums, and these
+ * times sm_scale stay below 2^127; softmax weights below 2^-126 of a head's largest
+ * count as zero.  sm_scale: up to 2^127 in magnitude (INVALID past it). */
 mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *cache, const void *q, float *out, float sm_scale,
                                              void *ws, size_t ws_bytes, void *stream);
 
@@ -658,8 +658,10 @@ mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *cache, c
  *   ws     : at least mosaic_nibble_workspace_bytes bytes, 256-byte aligned
  * Softmax weights are rounded to the dtype before their product with V (below
  * 2^-35 of a row's largest in fp16, 2^-126 in bf16, they count as zero).
- * sm_scale: any finite number.  A query that attends nothing gets zeros.  q, K and V as long as a head's products and
- * the sums of weights times values stay within fp32.
+ * sm_scale: up to 2^127 in magnitude (INVALID past it).  A query that attends
+ * nothing gets zeros.  q and K as long as a head's products, their sums, and these
+ * times sm_scale stay below 2^127, V as long as the sums of weights times values
+ * stay within fp32.
  * Errors: INVALID, UNSUPPORTED (head_dim, block_len, max_new past 2^27 or 2^23
  * tiles of 32 rows). */
 mosaic_status mosaic_nibble_attend(const mosaic_nibble_cache *cache, const void *q, void *out, const int64_t *q_strides_host,

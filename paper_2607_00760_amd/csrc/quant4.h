@@ -57,6 +57,11 @@ template <int DT> __device__ __forceinline__ uint32_t pack16(float a, float b) {
         return __builtin_bit_cast(uint32_t, r);
     }
 }
+// The softmax scale in powers of two, positive (a negative one's sign goes to the
+// query), as logits are scaled when their maximum is known.  A scale of zero is one
+// of a query of zeros: a masked logit, minus infinity, times zero would be NaN.
+__device__ __forceinline__ float powers_of(float scale) { return scale == 0.0f ? 1.0f : fabsf(scale) * 1.44269504088896340736f; }
+__device__ __forceinline__ uint32_t flip_of(float scale) { return scale < 0.0f ? 0x80008000u : 0u; }
 // element i of 16-bit pairs
 template <int DT> __device__ __forceinline__ float half_of(const uint32_t *w, int i) {
     return h2f((uint16_t)((i & 1) ? w[i >> 1] >> 16 : w[i >> 1]), DT);

@@ -146,12 +146,11 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
 #pragma unroll
     for (int e = 0; e < 4; ++e) qw[e] = *(const uint4 *)(qp + 32 * q4 + 8 * e);
     if (t < b1) load(t, st0);
-    // softmax scale in powers of two, positive (a negative one's sign goes to the
-    // query), as logits are scaled when their maximum is known
-    const float zs = fmaxf(fabsf(scale) * 1.44269504088896340736f, 0x1p-120f);
-    const uint32_t flip = scale < 0.0f ? 0x80008000u : 0u;
+    const float zs = powers_of(scale);
+    const uint32_t flip = flip_of(scale), keep = scale == 0.0f ? 0u : ~0u;
+    auto scaled = [&](uint4 w) { return make_uint4((w.x & keep) ^ flip, (w.y & keep) ^ flip, (w.z & keep) ^ flip, (w.w & keep) ^ flip); };
 #pragma unroll
-    for (int e = 0; e < 4; ++e) qw[e] = make_uint4(qw[e].x ^ flip, qw[e].y ^ flip, qw[e].z ^ flip, qw[e].w ^ flip);
+    for (int e = 0; e < 4; ++e) qw[e] = scaled(qw[e]);
     // the part of the query's products that the lane's column holds
     const int mypart = GP == 8 ? l16 >> 3 : (DT ? (l16 >> 2) & 1 : l16 >> 2);
     const uint32_t qh1 = mypart >= 1 ? 0xffff0000u : 0u, qh2 = mypart >= 2 ? 0xffff0000u : 0u, qh3 = mypart >= 3 ? 0u : ~0u;
@@ -339,8 +338,7 @@ k_quant4_attn(Q4Cache q, const uint16_t *query, float scale, uint32_t *arrivals,
         M8 qd[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint4 w = *(const uint4 *)(qp + 32 * e + 8 * q4);
-            const uint4 f = make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip);
+            const uint4 f = scaled(*(const uint4 *)(qp + 32 * e + 8 * q4));
             __builtin_memcpy(&qd[e], &f, 16);
         }
         uint4 vt[NS][8];                                   // (rows behind the last token may hold anything)

@@ -342,12 +342,13 @@ template <int DT> struct Rows {
         const int qi = row / q.G, head = pl.h * q.G + row - qi * q.G;
         valid = qi < pl.m;
         seen = valid ? (c.causal ? pl.L - pl.m + qi + 1 : pl.L) : 0;
-        zs = fmaxf(fabsf(c.scale) * 1.44269504088896340736f, 0x1p-120f);  // (0: every logit's power is 1; a masked one's is not)
+        zs = powers_of(c.scale);
         const uint16_t *qp = c.q + pl.s * c.q_seq + qi * c.q_tok + head * c.q_head + 8 * hl;
-        const uint32_t flip = c.scale < 0.0f ? 0x80008000u : 0u;
+        const uint32_t flip = flip_of(c.scale);
+        const bool live = valid && c.scale != 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint4 w = valid ? *(const uint4 *)(qp + 16 * e) : make_uint4(0, 0, 0, 0);
+            const uint4 w = live ? *(const uint4 *)(qp + 16 * e) : make_uint4(0, 0, 0, 0);
             qf[e] = dealt<DT>(make_uint4(w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip));
         }
 #pragma unroll

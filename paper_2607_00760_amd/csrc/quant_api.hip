@@ -137,6 +137,9 @@ mosaic_status quant4_ws_args(const mosaic_nibble_cache *c, const void *ws, size_
     return MOSAIC_OK;
 }
 
+// a softmax scale that is finite in powers of two, too
+bool scale_fits(float sm_scale) { return std::fabs(sm_scale) <= 0x1p127f; }
+
 // strides of a tensor of n0 x n1 x n2 rows that leave some row misaligned (the
 // stride of a dimension of one row may be anything)
 bool bad_strides(const int64_t *s, int n0, int n1, int n2) {
@@ -334,7 +337,7 @@ mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *c, const
     if (st != MOSAIC_OK) return st;
     if (!q || !out || !ws) return fail(MOSAIC_ERR_INVALID, "NULL argument");
     if (off16(q) || off16(out)) return fail(MOSAIC_ERR_INVALID, "q and out must be 16-byte aligned");
-    if (!std::isfinite(sm_scale)) return fail(MOSAIC_ERR_INVALID, "sm_scale not finite");
+    if (!scale_fits(sm_scale)) return fail(MOSAIC_ERR_INVALID, "sm_scale %g: at most 2^127 in magnitude", (double)sm_scale);
     const mosaic_status sw = quant4_ws_args(c, ws, ws_bytes);
     if (sw != MOSAIC_OK) return sw;
     return done(launch_quant4_attn(qc, c->block_len, c->dtype, (const uint16_t *)q, sm_scale, ws, out, (hipStream_t)stream), "attention launch");
@@ -353,7 +356,7 @@ mosaic_status mosaic_nibble_attend(const mosaic_nibble_cache *c, const void *q, 
         return fail(MOSAIC_ERR_INVALID, "q/out must be 16-byte aligned, their strides multiples of 8 elements");
     if (rows_overlap(out_strides, S, max_new, heads)) return fail(MOSAIC_ERR_INVALID, "rows of an output overlap");
     if ((uintptr_t)new_lens % 4) return fail(MOSAIC_ERR_INVALID, "new_lens must be 4-byte aligned");
-    if (!std::isfinite(sm_scale)) return fail(MOSAIC_ERR_INVALID, "sm_scale not finite");
+    if (!scale_fits(sm_scale)) return fail(MOSAIC_ERR_INVALID, "sm_scale %g: at most 2^127 in magnitude", (double)sm_scale);
     const mosaic_status sw = quant4_ws_args(c, ws, ws_bytes);
     if (sw != MOSAIC_OK) return sw;
     if (max_new == 0) return done(hipSuccess, "");
