@@ -657,11 +657,11 @@ mosaic_status mosaic_nibble_decode_attention(const mosaic_nibble_cache *cache, c
  *            overlap, out may be q (same pointer and strides)
  *   ws     : at least mosaic_nibble_workspace_bytes bytes, 256-byte aligned
  * Softmax weights are rounded to the dtype before their product with V (below
- * 2^-35 of a row's largest in fp16, 2^-126 in bf16, they count as zero).
+ * 2^-35 of a row's largest in fp16, 2^-118 in bf16, they count as zero).
  * sm_scale: up to 2^127 in magnitude (INVALID past it).  A query that attends
  * nothing gets zeros.  q and K as long as a head's products, their sums, and these
- * times sm_scale stay below 2^127, V as long as the sums of weights times values
- * stay within fp32.
+ * times sm_scale stay below 2^127, V as long as its largest magnitude times the
+ * tokens attended stays within fp32.
  * Errors: INVALID, UNSUPPORTED (head_dim, block_len, max_new past 2^27 or 2^23
  * tiles of 32 rows). */
 mosaic_status mosaic_nibble_attend(const mosaic_nibble_cache *cache, const void *q, void *out, const int64_t *q_strides_host,

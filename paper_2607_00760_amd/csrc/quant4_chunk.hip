@@ -40,12 +40,14 @@ constexpr int CK_ROWS = 256;                               // rows of a workgrou
 constexpr int CK_FEW = 32, CK_FEW_WAVES = 8;
 constexpr int CK_LEAST = 4;                                // steps of a share at least (of few rows: one for each wave)
 
-// Weights of fp16 are this power of two times as large: those of 2^-25 and less
-// of the row's largest would vanish, and a million of them count.  The running
+// Weights are this power of two times as large.  fp16: those of 2^-25 and less of
+// the row's largest would vanish, and a million of them count.  bf16: the running
 // maximum is left behind by up to CK_LAG powers of two, as sums are multiplied
-// through when it moves.
-template <int DT> constexpr float CK_POW = DT ? 0.0f : 10.0f;
+// through when it moves, and a weight past 1 times a value next to the type's
+// largest would be infinite.
+template <int DT> constexpr float CK_POW = DT ? -8.0f : 10.0f;
 template <int DT> constexpr float CK_LAG = DT ? 8.0f : 4.0f;
+static_assert(CK_POW<1> + CK_LAG<1> <= 0.0f, "bf16 weights are at most 1");
 
 typedef __attribute__((ext_vector_type(16))) float cf16;
 typedef __attribute__((ext_vector_type(2))) float cf2;
