@@ -527,8 +527,9 @@ class _BlockCache:
         self.elem = torch.bfloat16 if params.dtype == "bf16" else torch.float16
         self.max_tokens = -(-max_tokens // params.block) * params.block
 
-    def _take(self, c, shapes, given, ws_bytes):
-        """The tensors (those given, or new ones) and the rest of the structure."""
+    def _take(self, c, shapes, given, ws_bytes, workspace):
+        """The tensors and the workspace (those given, or new ones) and the rest of
+        the structure."""
         import torch
         self._c = c
         S, H = self.num_seqs, self.params.num_kv_heads
@@ -549,9 +550,15 @@ class _BlockCache:
         c.refused = self.refused.data_ptr()
         self._arrivals = torch.zeros((S, H, 32), dtype=torch.int32, device=self.device)
         c.arrivals = self._arrivals.data_ptr()
-        self.workspace = torch.zeros(n.value, dtype=torch.uint8, device=self.device)
+        if workspace is None:
+            workspace = torch.zeros(n.value, dtype=torch.uint8, device=self.device)
+        _check_tensor(workspace, "workspace", torch.uint8, self.device)
+        if workspace.numel() < n.value or workspace.data_ptr() % 256:
+            raise ValueError(f"workspace: {workspace.numel()} bytes at {workspace.data_ptr():#x}, expected {n.value} or more, 256-byte aligned")
+        #: scratch memory of the attention, zeros in its first 512 KiB between calls
+        self.workspace = workspace
         self._cp = C.byref(c)
-        self._ws = (self.workspace.data_ptr(), n.value)
+        self._ws = (workspace.data_ptr(), n.value)
         self._q_shape = (S, H * self.params.group_size, D)
 
     def tensors(self) -> dict:
@@ -673,11 +680,14 @@ class QuantCache(_BlockCache):
     some).  Lengths live on the device: nothing here synchronizes, and captured
     calls follow them.  Attention takes one query token a sequence, and outputs
     carry no gradient.  Calls on one cache must be ordered (one stream, or
-    events); they share its workspace."""
+    events); they share its workspace.  workspace:
+    another cache's (its attribute), or a tensor of enough bytes whose first 512
+    KiB are zero, to use in place of a new one; calls on all caches of one
+    workspace must be ordered."""
 
     TENSORS = ("k", "v", "k_scale", "v_scale", "bound_scale", "bounds", "k_tail", "v_tail", "lens")
 
-    def __init__(self, params: QuantParams, num_seqs: int, max_tokens: int, device="cuda", tensors=None):
+    def __init__(self, params: QuantParams, num_seqs: int, max_tokens: int, device="cuda", tensors=None, workspace=None):
         import torch
         given = dict(tensors or {})
         if params.format not in ("e4m3", "int8"):
@@ -691,7 +701,7 @@ class QuantCache(_BlockCache):
         lib = self.lib
         self._append, self._read, self._decode = lib.mosaic_quant_append, lib.mosaic_quant_read, lib.mosaic_quant_decode_attention
         self._take(MosaicQuantCache(S, H, params.group_size, D, 1 if params.dtype == "bf16" else 0, 1 if params.format == "int8" else 0, B, N),
-                   shapes, given, lib.mosaic_quant_workspace_bytes)
+                   shapes, given, lib.mosaic_quant_workspace_bytes, workspace)
 
     def decode_selected(self, q, sm_scale: float, select=(1, 10), out=None, blocks=None):
         """Attention over the share select = (num, den) of each (sequence, kv
@@ -734,11 +744,14 @@ class Quant4Cache(_BlockCache):
     tensors: a dict of these to use in place of new ones (all, or some).
     Lengths live on the device: nothing here synchronizes, and captured calls
     follow them.  Outputs carry no gradient.  Calls on one cache must be ordered
-    (one stream, or events); they share its workspace."""
+    (one stream, or events); they share its workspace.  workspace:
+    another cache's (its attribute), or a tensor of enough bytes whose first 512
+    KiB are zero, to use in place of a new one; calls on all caches of one
+    workspace must be ordered."""
 
     TENSORS = ("k", "v", "k_grid", "v_grid", "k_tail", "v_tail", "lens")
 
-    def __init__(self, params: Quant4Params, num_seqs: int, max_tokens: int, device="cuda", tensors=None):
+    def __init__(self, params: Quant4Params, num_seqs: int, max_tokens: int, device="cuda", tensors=None, workspace=None):
         import torch
         given = dict(tensors or {})
         self._make(params, num_seqs, max_tokens, device, given)
@@ -748,7 +761,7 @@ class Quant4Cache(_BlockCache):
         lib = self.lib
         self._append, self._read, self._decode = lib.mosaic_nibble_append, lib.mosaic_nibble_read, lib.mosaic_nibble_decode_attention
         self._take(MosaicNibbleCache(S, H, params.group_size, D, 1 if params.dtype == "bf16" else 0, B, N, 0), shapes, given,
-                   lib.mosaic_nibble_workspace_bytes)
+                   lib.mosaic_nibble_workspace_bytes, workspace)
 
     def attend(self, q, sm_scale: float, new_lens=None, causal: bool = True, out=None):
         """Attention of several query tokens of each sequence: q [S][n][H * G]

@@ -72,7 +72,7 @@ hipError_t launch_quant4_append(const Q4Cache &q, int block, int dtype, const QN
 size_t quant4_attn_ws_bytes(int pairs);
 hipError_t launch_quant4_attn(const Q4Cache &q, int block, int dtype, const uint16_t *query, float scale, void *ws, float *out,
                               hipStream_t s);
-size_t quant4_chunk_ws_bytes();
+size_t quant4_chunk_ws_bytes(int pairs, int blocks, int block);
 hipError_t launch_quant4_chunk(const Q4Cache &q, int block, int dtype, const QChunk &c, float *part, hipStream_t s);
 hipError_t launch_quant4_read(const Q4Cache &q, int block, int dtype, const QOut &o, hipStream_t s);
 hipError_t launch_quant_read(const QCache &q, int fmt, int block, int dtype, const QOut &o, hipStream_t s);

@@ -686,7 +686,11 @@ __global__ void __launch_bounds__(256) k_chunk_join(Q4Cache q, QChunk c, int til
 
 }  // namespace
 
-size_t quant4_chunk_ws_bytes() { return (size_t)CK_SLOTS * (CK_ROWS * (D + 4) * sizeof(float) + sizeof(int2)); }
+size_t quant4_chunk_ws_bytes(int pairs, int blocks, int block) {
+    // (nothing where no launch shares its tiles: as many pairs as slots, or tokens for one share)
+    if (pairs >= CK_SLOTS || ceil_div(blocks, CK_TILE / block) <= CK_LEAST) return 0;
+    return (size_t)CK_SLOTS * (CK_ROWS * (D + 4) * sizeof(float) + sizeof(int2));
+}
 
 hipError_t launch_quant4_chunk(const Q4Cache &q, int block, int dtype, const QChunk &c, float *part, hipStream_t s) {
     const int pairs = q.S * q.H, all = c.n * q.G;

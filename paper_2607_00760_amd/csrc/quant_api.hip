@@ -125,8 +125,9 @@ mosaic_status quant4_arrays(const mosaic_nibble_cache *c, Q4Cache &q) {
 struct Quant4Ws { uint64_t chunk, total; };
 Quant4Ws quant4_ws(const mosaic_nibble_cache *c) {
     Quant4Ws w;
-    w.chunk = align256(quant4_attn_ws_bytes(c->num_seqs * c->num_kv_heads));
-    w.total = w.chunk + align256(quant4_chunk_ws_bytes());
+    const int pairs = c->num_seqs * c->num_kv_heads;
+    w.chunk = align256(quant4_attn_ws_bytes(pairs));
+    w.total = w.chunk + align256(quant4_chunk_ws_bytes(pairs, c->max_blocks, c->block_len));
     return w;
 }
 
