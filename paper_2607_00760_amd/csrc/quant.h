@@ -1,6 +1,6 @@
 // quant.h -- shared by the kernels of the 8-bit KV cache (quant_append.hip,
-// quant_attn.h, quant_select.hip) and by their entry points (quant_api.hip)
-// (not part of the C ABI).
+// quant_attn.h, quant_select.hip), by those of the 4-bit one (quant4.h) and by
+// their entry points (quant_api.hip) (not part of the C ABI).
 #pragma once
 #include "decode_common.h"
 
@@ -95,6 +95,10 @@ __host__ __device__ __forceinline__ int q_want(int whole, int num, int den) {
     const long long n = ((long long)whole * num + den - 1) / den;
     return (int)(n < 1 ? (whole < 1 ? whole : 1) : (n > whole ? whole : n));
 }
+
+// what weights that sum to s are multiplied by in an average.  (Averages are
+// joined, not sums: a sum of values next to the type's largest overflows.)
+__device__ __forceinline__ float share_of(float s) { return s > 0.0f ? 1.0f / s : (s != s ? s : 0.0f); }
 
 struct QSel {                                              // a selection, or list = null: every block
     int num, den;

@@ -385,22 +385,22 @@ template <int DT> struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) z[i & 1] = mma32<DT>(x[i], qf[2 * g + (i >> 1)], z[i & 1]);
     }
-    // outputs of the weights pf over the values at vl, and the logits z[n][i] of token 32 n + 16 (i / 8) + 8 hl + i % 8 of
-    // the keys at kl; what an instruction takes is read while the four before it run
-    template <bool V, bool K> __device__ __forceinline__ void multiply(const uint8_t *vl, const uint4 (&pf)[4], const uint8_t *kl, int lane, cf16 (&z)[2]) {
+    // outputs of the weights pf over the values at `at` (V), or the logits z[n][i] of
+    // token 32 n + 16 (i / 8) + 8 hl + i % 8 of the keys there; what an instruction
+    // takes is read while the four before it run
+    template <bool V> __device__ __forceinline__ void multiply(const uint8_t *at, const uint4 (&pf)[4], int lane, cf16 (&z)[2]) {
         uint4 x[2][4];
-        if (V) read_v(vl, lane, 0, x[0]); else read_k(kl, lane, 0, x[0]);
-        if (K)
+        if (V) read_v(at, lane, 0, x[0]); else read_k(at, lane, 0, x[0]);
+        if (!V)
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) z[n][i] = 0.0f;
 #pragma unroll
-        for (int g = V ? 0 : 4; g < (K ? 8 : 4); ++g) {
-            if (g + 1 < 4) read_v(vl, lane, g + 1, x[(g + 1) & 1]);
-            else if (g + 1 < (K ? 8 : 4)) read_k(kl, lane, g + 1 - 4, x[(g + 1) & 1]);
+        for (int g = 0; g < 4; ++g) {
+            if (g < 3) { if (V) read_v(at, lane, g + 1, x[(g + 1) & 1]); else read_k(at, lane, g + 1, x[(g + 1) & 1]); }
             __builtin_amdgcn_sched_barrier(0);
-            if (g < 4) mul_v(x[g & 1], pf[g]); else mul_k(x[g & 1], g - 4, z);
+            if (V) mul_v(x[g & 1], pf[g]); else mul_k(x[g & 1], g, z);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -470,7 +470,6 @@ template <int DT> struct Rows {
     }
 };
 
-__device__ __forceinline__ float share_of(float s) { return s > 0.0f ? 1.0f / s : (s != s ? s : 0.0f); }
 __device__ __forceinline__ uint16_t *out_row(const Q4Cache &q, const QChunk &c, const ChunkPlan &pl, int row) {
     const int qi = row / q.G, head = pl.h * q.G + row - qi * q.G;
     return c.out + pl.s * c.o_seq + qi * c.o_tok + head * c.o_head;
@@ -528,18 +527,18 @@ k_chunk(Q4Cache q, QChunk c, int tiles, int shared, float *part) {
         for (; i < plain; ++i) {
             lds_barrier();
             if (VALS) { store_full(i + 1); load(i + 2); }
-            r.template multiply<false, true>(nullptr, pf, kl[i & 1], lane, z);
+            r.template multiply<false>(kl[i & 1], pf, lane, z);
             if (!VALS) { store_full(i + 1); load(i + 2); }
             r.weigh(z, t0 + i, hl, false, pf);
-            r.template multiply<true, false>(vl[i & 1], pf, nullptr, lane, z);
+            r.template multiply<true>(vl[i & 1], pf, lane, z);
         }
         for (; i < n; ++i) {
             lds_barrier();
             if (VALS) { store(i + 1); load(i + 2); }
-            r.template multiply<false, true>(nullptr, pf, kl[i & 1], lane, z);
+            r.template multiply<false>(kl[i & 1], pf, lane, z);
             if (!VALS) { store(i + 1); load(i + 2); }
             r.weigh(z, t0 + i, hl, CK_TILE * (t0 + i + 1) > all, pf);
-            r.template multiply<true, false>(vl[i & 1], pf, nullptr, lane, z);
+            r.template multiply<true>(vl[i & 1], pf, lane, z);
         }
     };
     if (n > 0) {

@@ -1,5 +1,5 @@
 // quant_join.h -- how the waves of a workgroup and the runs of a pair of the
-// caches' decode attentions are joined (quant_attn.h, quant4_attn.h).
+// caches' decode attentions are joined (quant_attn.h, quant4_attn.hip).
 #pragma once
 #include "quant.h"
 
@@ -10,10 +10,6 @@ namespace {
 constexpr int QA_NWV = 4;                                  // waves of a workgroup
 constexpr int QA_HEADS = 8;
 constexpr int QA_PART = QA_HEADS * (D + 2);                // floats of a partial: (max, sum) and averages of the heads
-
-// what weights that sum to s are multiplied by in an average.  (Averages are
-// joined, not sums: a sum of values next to the type's largest overflows.)
-__device__ __forceinline__ float share_of(float s) { return s > 0.0f ? 1.0f / s : (s != s ? s : 0.0f); }
 
 // partials, past the XCD's L2
 __device__ __forceinline__ void put2(float *p, float2 x) {
