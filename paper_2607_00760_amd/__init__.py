@@ -769,8 +769,10 @@ class Quant4Cache(_BlockCache):
         channels.  new_lens: int32 [S] on the GPU, how many of its n queries each
         sequence has (None: all).  causal: they are its last tokens (in the cache
         by then), and each attends the tokens up to itself; otherwise each
-        attends every token.  The tokens are those that read() gives.  Rows past
-        new_lens are neither read nor written (zeros in a new tensor)."""
+        attends every token.  The tokens are those that read() gives.  Weights
+        are rounded to the cache's type before their product with the values, as
+        the results are (decode keeps 22 bits of them).  Rows past new_lens are
+        neither read nor written (zeros in a new tensor)."""
         import torch
         S, heads = self.num_seqs, self._q_shape[1]
         if not isinstance(q, torch.Tensor) or q.dim() != 4:

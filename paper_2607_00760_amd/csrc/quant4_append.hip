@@ -14,7 +14,8 @@
 // A token's least and largest value meet in its 16 lanes, a channel's in LDS,
 // where one thread a channel makes the grid.  HBM is the bound: 512 bytes of a
 // token are read, 128 and its share of the grids are written (4 x 32785 tokens of 8
-// heads, 0.69 GB: 119 us, 5.8 TB/s).
+// heads, 0.69 GB: 119 us, 5.8 TB/s).  One token of 8 or 64 sequences, 8 heads: 2.7
+// and 3.6 us in a captured step, a launch and one chain of round trips.
 #include <type_traits>
 
 #include "quant4.h"
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(8 * B) k_quant4_append(Q4Cache q, QNew nw) {
         if (j * B >= f) {                                  // new tokens only
             const uint16_t *row = src + (int64_t)(j * B - f + t0) * tok + 8 * pc;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {                      // (streamed: 4 x 32785 tokens of 8 heads 257 us, 275 without)
+            for (int r = 0; r < 4; ++r) {                      // (streamed: 4 x 32785 tokens written and read back 257 us, 275 without)
                 x[r] = __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4 *)row));
                 row += step * tok;
             }

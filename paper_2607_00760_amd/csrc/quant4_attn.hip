@@ -24,7 +24,9 @@
 // TB/s, a copy's rate being 4.95, with the vector ALU 65 % busy; 16 ragged
 // sequences of up to 96 K tokens, 4 heads, groups of 7, blocks of 32 (0.57 GB) 149
 // us, 3.8 TB/s: eight rows of weights a code instead of four and grids twice as
-// often, so the ALU is the bound.  One sequence of 4117 tokens 10.5 us, a chain of
+// often, so the ALU is the bound.  fp16, groups of 5 to 8, has the third parts of the
+// query in a product of their own: the ragged case 168 us, 8 x 128 K with groups of 8
+// 279.  One sequence of 4117 tokens 10.5 us, a chain of
 // plan, query, two steps and joins.
 //
 // The second sum is in units of a power of two that follows the largest product

@@ -17,8 +17,12 @@
 // heads, 1.07 TFLOP, causal) take 991 to 1044 us, 1.02 to 1.07 PFLOP/s; a bf16 product of 8192^3
 // reaches 1.25.  The matrix unit is busy 55 % of the cycles, at 1.9 GHz of 2.4: the
 // card's power holds the clock down, and codes are worked out and weights made
-// meanwhile.  Few rows: 5 queries over 8 x 32 K tokens take 89 us, 3.3 TB/s: a
-// wave's codes, logits, weights and outputs are one chain, two waves a SIMD.
+// meanwhile.  Few rows: 5 queries over 8 x 32 K tokens take 88 to 92 us, 3.2 to 3.3
+// TB/s: a step is some 830 vector instructions of a wave, 640 of them to work out the
+// values, 45 us of issue beside the 59 of a copy's rate; and a wave's codes, logits,
+// weights and outputs are one chain, two waves a SIMD.  33 to 128 rows are between
+// these: 9 to 16 queries over the same tokens take 195 us, one wave a SIMD, and
+// waves without rows multiply as the others do.
 //
 // Rows are many or few.  Many: all waves of a workgroup share 64 tokens, worked
 // out a step ahead into the other half of LDS.  At most 32 (k_chunk_few): each
